@@ -14,6 +14,13 @@
  *   dense_attention    Preliminaries, first equation (softmax(QK^T/sqrt d)V), the
  *                      speed-up baseline, written with the same tile loop
  *
+ * and, beside dense_attention, exact attention as language and packed-sequence models have it:
+ *   pisa_masked_attention            documents, prefix, causal rows, capped and distance-biased
+ *                                    scores, shared key heads, strided tensors
+ *   pisa_masked_attention_backward   its gradients
+ *   pisa_paged_append                new tokens' keys and values into a paged cache
+ *   pisa_paged_attention             one new token per sequence over that cache
+ *
  * Conventions
  *   - All tensor pointers are DEVICE pointers owned by the caller; the library never
  *     allocates, frees or synchronises.  Work is enqueued on `stream`
@@ -230,6 +237,135 @@ int32_t pisa_forward(const pisa_shape* shape, const void* q, const void* k, cons
  * 64-key tiles; lse as above (may be NULL).  shape->block only sets the tile walk. */
 int32_t dense_attention(const pisa_shape* shape, const void* q, const void* k, const void* v,
                         void* out, float* lse, void* stream);
+
+/*
+ * Exact attention with masks.  For every batch element b, query head h and query row i, at position
+ * pos_i = i + kv_len - q_len (the query rows are the last q_len of the kv_len positions):
+ *   z_ij  = s_ij = scale q_i . k_j                           (softcap == 0)
+ *   z_ij  = softcap tanh(s_ij / softcap)                     (softcap > 0)
+ *   z_ij -= slopes[h] |pos_i - j|                            (slopes given)
+ *   out_i = sum_j p_ij v_j,  p_ij = exp(z_ij - lse_i),  lse_i = log sum_j exp(z_ij),  j over the keys that row i sees.
+ * Key head of query head h: h / (heads / kv_heads).
+ * Which keys a row sees, all of them intervals:
+ *   num_docs == 0: keys 0 .. kv_len-1; with causal, keys 0 .. max(pos_i, prefix[b] - 1).
+ *   num_docs > 0:  document c of batch element b holds positions doc_offsets[b][c] .. doc_offsets[b][c+1]-1 (ascending;
+ *                  equal neighbours are an empty document; what lies before the first or behind the last offset is
+ *                  padding).  A row sees the keys of its own document; with causal, those up to
+ *                  max(pos_i, doc_offsets[b][c] + prefix[b][c] - 1).
+ * A row that sees no key has out = 0 and lse = -inf (and gradients of 0; keys no row sees have gradients of 0 as well).
+ * What a row does not see does not reach it, whatever it holds: keys and values of infinity or NaN that are masked for
+ * row i, and query rows of infinity or NaN that do not see key j, leave out_i and the gradients of key j as they are.
+ * Strides are counted in elements, the channels of a row lie together; every stride has to be a multiple of 16 bytes
+ * and no negative number, a token stride below 2^31 / 64 bytes.  Batch or head strides of 0 are allowed for inputs
+ * (one tensor for all), not for outputs of more than one batch element or head.  All strides 0: dense
+ * [batch, heads, len, head_dim].
+ * doc_offsets and prefix are read on the device.  Offsets that do not ascend give rows other keys, but no access outside
+ * the tensors.
+ */
+typedef struct pisa_strides {
+  int64_t batch, head, token;
+} pisa_strides;
+
+typedef struct pisa_masked_shape {
+  int32_t batch;       /* >= 1 */
+  int32_t heads;       /* query heads, a multiple of kv_heads */
+  int32_t kv_heads;    /* >= 1 */
+  int32_t q_len;       /* >= 1 */
+  int32_t kv_len;      /* 0 .. 2^24; k and v may be NULL at 0 */
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t dtype;       /* PISA_FP32 or PISA_BF16: element type of all tensors but lse, slopes, doc_offsets, prefix */
+  int32_t causal;      /* 0 or 1 */
+  int32_t num_docs;    /* >= 0; 0: doc_offsets is NULL */
+  float   scale;       /* <= 0 selects 1/sqrt(head_dim) */
+  float   softcap;     /* >= 0; 0: scores are not capped */
+  pisa_strides q, k, v, out;
+} pisa_masked_shape;
+
+/*
+ *   q [batch, heads, q_len, d], k, v [batch, kv_heads, kv_len, d], out as q: device, strided as the shape says
+ *   doc_offsets int32 [batch, num_docs + 1], NULL if num_docs == 0
+ *   prefix   int32 [batch, max(num_docs, 1)], tokens at the start of each document that all of its rows see (negative
+ *            counts as 0, more than the document as all of it); may be NULL; causal only
+ *   slopes   fp32 [heads], may be NULL
+ *   lse      fp32 [batch, heads, q_len], may be NULL
+ *   workspace  pisa_masked_attention_workspace_bytes(shape) bytes, 16-byte aligned (may be NULL if that is 0): where there
+ *            are few query rows their keys are shared out among workgroups and the parts joined from there
+ * Two calls on different streams need a workspace each.
+ */
+size_t pisa_masked_attention_workspace_bytes(const pisa_masked_shape* shape);    /* 0 for an invalid shape as well */
+int32_t pisa_masked_attention(const pisa_masked_shape* shape, const void* q, const void* k, const void* v,
+                              const int32_t* doc_offsets, const int32_t* prefix, const float* slopes,
+                              void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of pisa_masked_attention with respect to q, k and v, from dout, the gradient of out:
+ *   delta_i = dout_i . out_i,  dz_ij = p_ij (dout_i . v_j - delta_i),  ds_ij = dz_ij (1 - tanh^2(s_ij / softcap)),
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i,
+ * the last two over the rows that see key j of all query heads that share its head.  slopes are constants here.  Sums are
+ * made in a fixed order: equal calls give equal bits.
+ *   out, lse  as pisa_masked_attention wrote them for the same arguments
+ *   strides   of dout, dq, dk, dv; NULL: those of out, q, k, v
+ *   dq, dk, dv  written, never read; in shape->dtype, sums in fp32, rounded once
+ *   workspace pisa_masked_attention_backward_workspace_bytes(shape) bytes, 16-byte aligned
+ */
+typedef struct pisa_grad_strides {
+  pisa_strides dout, dq, dk, dv;
+} pisa_grad_strides;
+size_t pisa_masked_attention_backward_workspace_bytes(const pisa_masked_shape* shape);
+int32_t pisa_masked_attention_backward(const pisa_masked_shape* shape, const pisa_grad_strides* strides,
+                                       const void* q, const void* k, const void* v, const void* out, const float* lse,
+                                       const void* dout, const int32_t* doc_offsets, const int32_t* prefix,
+                                       const float* slopes, void* dq, void* dk, void* dv,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A paged cache: position pos of sequence s lies in slot pos % page_size of page page_table[s][pos / page_size] of
+ * k_pages and v_pages, tensors of num_pages pages that the strides describe (batch: from page to page, token: from slot to
+ * slot), so [num_pages, page_size, kv_heads, d] and [num_pages, kv_heads, page_size, d] are both taken.
+ * lengths[s] is the number of cached tokens; a length below 0 counts as 0, one above max_pages * page_size as that.
+ * Page numbers outside [0, num_pages) are never followed: what belongs to them is not written, and not attended to.
+ */
+typedef struct pisa_paged_shape {
+  int32_t seqs;        /* >= 1 */
+  int32_t heads;       /* query heads, a multiple of kv_heads */
+  int32_t kv_heads;    /* >= 1 */
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t dtype;       /* PISA_FP32 or PISA_BF16 */
+  int32_t page_size;   /* 1 .. 65536 */
+  int32_t num_pages;   /* >= 1 */
+  int32_t max_pages;   /* >= 1: entries in a row of page_table; max_pages * page_size <= 2^30 */
+  float   scale;       /* <= 0 selects 1/sqrt(head_dim) */
+  float   softcap;     /* >= 0; 0: none */
+  pisa_strides k_pages, v_pages;   /* all 0: dense [num_pages, page_size, kv_heads, d] */
+} pisa_paged_shape;
+
+/*
+ * Writes new tokens into the cache: rows offsets[s] .. offsets[s+1]-1 of k and v become the last tokens of sequence s,
+ * positions lengths[s] - (offsets[s+1] - offsets[s]) .. lengths[s] - 1; lengths already count them.  Rows outside
+ * [offsets[0], offsets[seqs]) and positions below 0 or past the table are not written anywhere.  Nothing else in the cache
+ * is touched.  Two rows for one slot (sequences that share a page) leave either.
+ *   k, v       [tokens, kv_heads, d], shape->dtype, dense;  tokens >= 0
+ *   offsets    int32 [seqs + 1], ascending, on the device
+ *   page_table int32 [seqs, max_pages], lengths int32 [seqs], on the device
+ */
+int32_t pisa_paged_append(const pisa_paged_shape* shape, const void* k, const void* v, int32_t tokens,
+                          const int32_t* offsets, void* k_pages, void* v_pages,
+                          const int32_t* page_table, const int32_t* lengths, void* stream);
+
+/*
+ * One query row per sequence and head, at position lengths[s] - 1, over all cached tokens of its sequence:
+ *   z_j = scale q . k_j, capped and biased by slopes[h] (lengths[s] - 1 - j) as in pisa_masked_attention,
+ *   out = sum_j exp(z_j - lse) v_j.  A sequence of length 0 has out = 0 and lse = -inf.
+ * The cached tokens of all sequences are shared out evenly among the workgroups, whatever their lengths, and the parts of a
+ * sequence joined in a fixed order.
+ *   q, out     [seqs, heads, d], shape->dtype, dense
+ *   lse        fp32 [seqs, heads], may be NULL;  slopes fp32 [heads], may be NULL
+ *   workspace  pisa_paged_attention_workspace_bytes(shape) bytes, 16-byte aligned
+ */
+size_t pisa_paged_attention_workspace_bytes(const pisa_paged_shape* shape);
+int32_t pisa_paged_attention(const pisa_paged_shape* shape, const void* q, const void* k_pages, const void* v_pages,
+                             const int32_t* page_table, const int32_t* lengths, const float* slopes,
+                             void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aid, not a step of the method: enqueues a register-only loop of the bf16

@@ -24,6 +24,9 @@ PISA_NORM_SPECTRAL, PISA_NORM_FROBENIUS, PISA_NORM_FROBENIUS_FAST = 0, 1, 2
 EXPORTS = ("pisa_num_blocks", "pisa_topk_count", "pisa_workspace_bytes", "pisa_block_stats",
            "pisa_block_heterogeneity", "pisa_select", "pisa_attention", "pisa_attention_static",
            "pisa_forward_workspace_bytes", "pisa_forward", "dense_attention",
+           "pisa_masked_attention_workspace_bytes", "pisa_masked_attention",
+           "pisa_masked_attention_backward_workspace_bytes", "pisa_masked_attention_backward",
+           "pisa_paged_append", "pisa_paged_attention_workspace_bytes", "pisa_paged_attention",
            "pisa_probe_mfma_rate", "pisa_probe_shader_clock", "pisa_last_error")
 
 
@@ -31,6 +34,28 @@ class PisaShape(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("seq_len", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
+
+
+class PisaStrides(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
+
+
+class PisaMaskedShape(ctypes.Structure):
+    _fields_ = [(x, ctypes.c_int32) for x in ("batch", "heads", "kv_heads", "q_len", "kv_len", "head_dim", "dtype", "causal",
+                                              "num_docs")] + \
+               [("scale", ctypes.c_float), ("softcap", ctypes.c_float)] + \
+               [(x, PisaStrides) for x in ("q", "k", "v", "out")]
+
+
+class PisaGradStrides(ctypes.Structure):
+    _fields_ = [(x, PisaStrides) for x in ("dout", "dq", "dk", "dv")]
+
+
+class PisaPagedShape(ctypes.Structure):
+    _fields_ = [(x, ctypes.c_int32) for x in ("seqs", "heads", "kv_heads", "head_dim", "dtype", "page_size", "num_pages",
+                                              "max_pages")] + \
+               [("scale", ctypes.c_float), ("softcap", ctypes.c_float)] + \
+               [(x, PisaStrides) for x in ("k_pages", "v_pages")]
 
 
 class PisaError(RuntimeError):
@@ -70,6 +95,21 @@ def _load() -> ctypes.CDLL:
     lib.pisa_forward.restype = i32
     lib.dense_attention.argtypes = [shp, vp, vp, vp, vp, vp, vp]
     lib.dense_attention.restype = i32
+    mshp, gstr, pshp = (ctypes.POINTER(x) for x in (PisaMaskedShape, PisaGradStrides, PisaPagedShape))
+    lib.pisa_masked_attention_workspace_bytes.argtypes = [mshp]
+    lib.pisa_masked_attention_workspace_bytes.restype = sz
+    lib.pisa_masked_attention.argtypes = [mshp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.pisa_masked_attention.restype = i32
+    lib.pisa_masked_attention_backward_workspace_bytes.argtypes = [mshp]
+    lib.pisa_masked_attention_backward_workspace_bytes.restype = sz
+    lib.pisa_masked_attention_backward.argtypes = [mshp, gstr] + [vp] * 13 + [sz, vp]
+    lib.pisa_masked_attention_backward.restype = i32
+    lib.pisa_paged_append.argtypes = [pshp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.pisa_paged_append.restype = i32
+    lib.pisa_paged_attention_workspace_bytes.argtypes = [pshp]
+    lib.pisa_paged_attention_workspace_bytes.restype = sz
+    lib.pisa_paged_attention.argtypes = [pshp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.pisa_paged_attention.restype = i32
     lib.pisa_probe_mfma_rate.argtypes = [i32, vp, sz, ctypes.POINTER(ctypes.c_double), vp]
     lib.pisa_probe_mfma_rate.restype = i32
     lib.pisa_probe_shader_clock.argtypes = [ctypes.c_double, vp, ctypes.POINTER(ctypes.c_double), vp]
@@ -263,6 +303,182 @@ def dense_attention(q, k, v, block: int = 64, scale: Optional[float] = None,
     _check(_lib.dense_attention(
         ctypes.byref(shape), _dev(q, "q"), _dev(k, "k", like=q), _dev(v, "v", like=q),
         _dev(out, "out", like=q), _dev(lse, "lse", torch.float32), _stream()))
+    return out, lse
+
+
+def _strides(t: torch.Tensor, name: str) -> PisaStrides:
+    """Of a [batch, heads, tokens, head_dim] view; the channels of a row have to lie together."""
+    b, h, n, c = t.stride()
+    if c != 1 and t.shape[3] > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return PisaStrides(b, h, n if t.shape[2] > 1 else max(n, t.shape[3]))
+
+
+def _same_device(ref: torch.Tensor, **others: Optional[torch.Tensor]) -> None:
+    if not ref.is_cuda:
+        raise ValueError("tensors must live on the GPU")
+    if ref.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors live on {ref.device}, the current device is cuda:{torch.cuda.current_device()}")
+    for name, t in others.items():
+        if t is not None and t.device != ref.device:
+            raise ValueError(f"{name} lives on {t.device}, q on {ref.device}")
+
+
+def _plain(t: Optional[torch.Tensor], name: str, dtype, shape) -> Optional[int]:
+    """Address of a dense tensor of a given type and shape."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _workspace(t: Optional[torch.Tensor], need: int, device) -> Tuple[Optional[torch.Tensor], int]:
+    if t is None:
+        t = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        return t, need
+    if not t.is_contiguous() or t.device != device:
+        raise ValueError("workspace must be contiguous and on the tensors' device")
+    return t, t.numel() * t.element_size()
+
+
+def _masked_shape(q, k, v, out, causal, doc_offsets, softcap, scale) -> PisaMaskedShape:
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("expected q, k, v of shape [batch, heads, tokens, head_dim]")
+    b, h, n, d = q.shape
+    if k.shape != v.shape or k.shape[0] != b or k.shape[3] != d:
+        raise ValueError(f"k and v must be alike and match q in batch and head_dim: {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)}")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise TypeError("q, k and v must have one dtype")
+    if out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must match q in shape and dtype")
+    docs = 0
+    if doc_offsets is not None:
+        if doc_offsets.dim() != 2 or doc_offsets.shape[1] < 2:
+            raise ValueError("doc_offsets must have shape [batch, documents + 1], with one document at least")
+        docs = doc_offsets.shape[1] - 1
+    return PisaMaskedShape(b, h, k.shape[1], n, k.shape[2], d, _dtype_code(q), 1 if causal else 0, docs,
+                           0.0 if scale is None else float(scale), float(softcap),
+                           _strides(q, "q"), _strides(k, "k"), _strides(v, "v"), _strides(out, "out"))
+
+
+def _mask_pointers(shape: PisaMaskedShape, doc_offsets, prefix, slopes):
+    return (_plain(doc_offsets, "doc_offsets", torch.int32, (shape.batch, shape.num_docs + 1)),
+            _plain(prefix, "prefix", torch.int32, (shape.batch, max(shape.num_docs, 1))),
+            _plain(slopes, "slopes", torch.float32, (shape.heads,)))
+
+
+def masked_attention(q, k, v, causal: bool = False, doc_offsets: Optional[torch.Tensor] = None,
+                     prefix: Optional[torch.Tensor] = None, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                     scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                     workspace: Optional[torch.Tensor] = None):
+    """pisa_masked_attention.  q [batch, heads, q_len, d], k and v [batch, kv_heads, kv_len, d], any strides with whole
+    rows of channels (a [batch, tokens, heads, d] tensor goes in as its transpose(1, 2)); doc_offsets int32
+    [batch, documents + 1], prefix int32 [batch, documents] (or [batch, 1]), slopes fp32 [heads].  Returns (out, lse or None);
+    `out` is laid out as q unless given."""
+    if out is None:
+        out = torch.empty_like(q)
+    shape = _masked_shape(q, k, v, out, causal, doc_offsets, softcap, scale)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+    _same_device(q, k=k, v=v, out=out, lse=lse, doc_offsets=doc_offsets, prefix=prefix, slopes=slopes)
+    docs, pre, slo = _mask_pointers(shape, doc_offsets, prefix, slopes)
+    workspace, size = _workspace(workspace, _lib.pisa_masked_attention_workspace_bytes(shape), q.device)
+    _check(_lib.pisa_masked_attention(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), docs, pre, slo, out.data_ptr(),
+                                      _plain(lse, "lse", torch.float32, q.shape[:3]),
+                                      None if workspace is None else workspace.data_ptr(), size, _stream()))
+    return out, lse
+
+
+def masked_attention_backward(q, k, v, out, lse, dout, causal: bool = False, doc_offsets: Optional[torch.Tensor] = None,
+                              prefix: Optional[torch.Tensor] = None, softcap: float = 0.0,
+                              slopes: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                              dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                              dv: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """pisa_masked_attention_backward: gradients of masked_attention(...) with the same arguments, from its out and lse and
+    the gradient dout of out.  Returns (dq, dk, dv)."""
+    dq, dk, dv = (torch.empty_like(x) if g is None else g for x, g in ((q, dq), (k, dk), (v, dv)))
+    shape = _masked_shape(q, k, v, out, causal, doc_offsets, softcap, scale)
+    for name, t, like in (("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+        if t.shape != like.shape or t.dtype != like.dtype:
+            raise ValueError(f"{name} must have shape {tuple(like.shape)} and dtype {like.dtype}")
+    strides = PisaGradStrides(_strides(dout, "dout"), _strides(dq, "dq"), _strides(dk, "dk"), _strides(dv, "dv"))
+    _same_device(q, k=k, v=v, out=out, lse=lse, dout=dout, doc_offsets=doc_offsets, prefix=prefix, slopes=slopes, dq=dq, dk=dk,
+                 dv=dv)
+    docs, pre, slo = _mask_pointers(shape, doc_offsets, prefix, slopes)
+    workspace, size = _workspace(workspace, _lib.pisa_masked_attention_backward_workspace_bytes(shape), q.device)
+    _check(_lib.pisa_masked_attention_backward(
+        shape, strides, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _plain(lse, "lse", torch.float32, q.shape[:3]),
+        dout.data_ptr(), docs, pre, slo, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+        None if workspace is None else workspace.data_ptr(), size, _stream()))
+    return dq, dk, dv
+
+
+def _page_strides(t: torch.Tensor, name: str) -> PisaStrides:
+    """Of a [pages, page_size, kv_heads, head_dim] view."""
+    p, n, h, c = t.stride()
+    if c != 1 and t.shape[3] > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return PisaStrides(p, h, n if t.shape[1] > 1 else max(n, t.shape[3]))
+
+
+def _paged_shape(k_pages, v_pages, page_table, heads, softcap, scale) -> PisaPagedShape:
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape:
+        raise ValueError("expected k_pages and v_pages of one shape [pages, page_size, kv_heads, head_dim]")
+    if v_pages.dtype != k_pages.dtype:
+        raise TypeError("k_pages and v_pages must have one dtype")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must have shape [sequences, pages of the longest]")
+    n, page, kvh, d = k_pages.shape
+    return PisaPagedShape(page_table.shape[0], heads, kvh, d, _dtype_code(k_pages), page, n, page_table.shape[1],
+                          0.0 if scale is None else float(scale), float(softcap),
+                          _page_strides(k_pages, "k_pages"), _page_strides(v_pages, "v_pages"))
+
+
+def paged_append(k, v, offsets, k_pages, v_pages, page_table, lengths) -> None:
+    """pisa_paged_append: rows offsets[s] .. offsets[s+1]-1 of k and v [tokens, kv_heads, d] become the last cached tokens of
+    sequence s, whose lengths[s] counts them already.  offsets int32 [sequences + 1], page_table int32 [sequences, pages],
+    lengths int32 [sequences]; k_pages and v_pages as for paged_attention, written in place."""
+    shape = _paged_shape(k_pages, v_pages, page_table, k_pages.shape[2] if k_pages.dim() == 4 else 0, 0.0, None)
+    _same_device(k_pages, v_pages=v_pages, k=k, v=v, offsets=offsets, page_table=page_table, lengths=lengths)
+    if k.dim() != 3:
+        raise ValueError("expected k and v of shape [tokens, kv_heads, head_dim]")
+    rows = (k.shape[0], shape.kv_heads, shape.head_dim)
+    _check(_lib.pisa_paged_append(
+        shape, _plain(k, "k", k_pages.dtype, rows), _plain(v, "v", k_pages.dtype, rows), k.shape[0],
+        _plain(offsets, "offsets", torch.int32, (shape.seqs + 1,)), k_pages.data_ptr(), v_pages.data_ptr(),
+        _plain(page_table, "page_table", torch.int32, page_table.shape),
+        _plain(lengths, "lengths", torch.int32, (shape.seqs,)), _stream()))
+
+
+def paged_attention(q, k_pages, v_pages, page_table, lengths, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                    scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, want_lse: bool = False,
+                    workspace: Optional[torch.Tensor] = None):
+    """pisa_paged_attention: one query row per sequence and head, q [sequences, heads, d], over a cache k_pages, v_pages
+    [pages, page_size, kv_heads, d] (any strides with whole rows of channels).  Returns (out, lse or None)."""
+    if q.dim() != 3:
+        raise ValueError("expected q of shape [sequences, heads, head_dim]")
+    if q.dtype != k_pages.dtype:
+        raise TypeError("q and the pages must have one dtype")
+    shape = _paged_shape(k_pages, v_pages, page_table, q.shape[1], softcap, scale)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    _same_device(q, k_pages=k_pages, v_pages=v_pages, page_table=page_table, lengths=lengths, slopes=slopes, out=out, lse=lse)
+    rows = (shape.seqs, shape.heads, shape.head_dim)
+    workspace, size = _workspace(workspace, _lib.pisa_paged_attention_workspace_bytes(shape), q.device)
+    _check(_lib.pisa_paged_attention(
+        shape, _plain(q, "q", q.dtype, rows), k_pages.data_ptr(), v_pages.data_ptr(),
+        _plain(page_table, "page_table", torch.int32, page_table.shape), _plain(lengths, "lengths", torch.int32, (shape.seqs,)),
+        _plain(slopes, "slopes", torch.float32, (shape.heads,)), _plain(out, "out", q.dtype, rows),
+        _plain(lse, "lse", torch.float32, q.shape[:2]), None if workspace is None else workspace.data_ptr(), size, _stream()))
     return out, lse
 
 

@@ -19,7 +19,8 @@ FOUR = ["-DPISA_ATTN_FOUR", "-mllvm", "-amdgpu-sched-strategy=max-memory-clause"
 UNITS = [("api.hip", "api", []), ("stats.hip", "stats", []), ("stats_bf16.hip", "stats_bf16", []),
          ("select.hip", "select", []), ("hetero.hip", "hetero", []), ("attn_fp32.hip", "attn_fp32", []),
          ("attn_bf16.hip", "attn_bf16", ITERATIVE), ("attn_bf16.hip", "attn_bf16_four", FOUR),
-         ("pairing.hip", "pairing", []), ("probe.hip", "probe", [])]
+         ("pairing.hip", "pairing", []), ("probe.hip", "probe", []), ("masked_api.hip", "masked_api", []),
+         ("masked_fwd.hip", "masked_fwd", []), ("masked_bwd.hip", "masked_bwd", []), ("paged.hip", "paged", [])]
 OBJ_DIR = os.path.join(PKG_DIR, "_build")
 
 

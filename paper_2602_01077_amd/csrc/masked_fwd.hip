@@ -1,0 +1,364 @@
+// Masked attention, forward: one pass over the keys that a row sees, with a running maximum and sum.
+//
+// A workgroup has 128 query rows, a wave 32 of them; all products are transposed, so a lane holds one query row:
+//     S^T (keys x rows) = K (keys x channels) Q^T,    O^T (channels x rows) += V^T (channels x keys) P^T
+// and a row's mask, an interval of keys, is two registers of its lane.  Key tiles of 64 rows go through LDS by DMA, two stages
+// each for K and V, one barrier a tile: behind it the loads of K(t+2) and V(t+1) go out, then the softmax of tile t,
+// O^T += V(t)^T P(t)^T and S^T(t+1).  The walk goes over the tiles that some row of the workgroup sees; a wave leaves out
+// those that none of its rows sees, and compares key numbers only in those that some of them see in part.
+#include "masked.h"
+#include "tile.h"
+
+namespace pisa {
+
+using namespace tile;
+
+namespace {
+
+constexpr int kQRows = 128;
+constexpr int CAP = 1, BIAS = 2;         // bits of MOD: scores capped, biased by distance
+
+struct Plan {
+  int n_qt;            // tiles of 128 rows to a head
+  int n_parts;         // workgroups that share a tile's keys
+  int total, per_xcd;  // items: (batch, head, tile, part)
+  float* part_o;       // n_parts > 1: [item][128][d] sums of weighted values, before division
+  float* part_ml;      // [item][2][128] maximum and sum of weights
+};
+
+template <typename T, int D> struct Row {        // what a lane holds of its query row
+  f32x16 o[Geo<T, D>::NDT];
+  float m, l;          // running maximum; this lane's share of the sum (keys with its h)
+};
+
+// The maximum takes in t (this lane's largest score); l and o are rescaled if some lane's moved.
+template <typename T, int D> __device__ inline void raise_max(Row<T, D>& st, float t) {
+  t = fmaxf(t, __shfl_xor(t, 32));
+  const float m = fmaxf(st.m, t);
+  if (__any(m != st.m)) {
+    const float f = st.m == -INFINITY ? 0.f : exp_of<T>(st.m - m);
+    st.l *= f;
+#pragma unroll
+    for (int dt = 0; dt < Geo<T, D>::NDT; ++dt) st.o[dt] *= f;
+    st.m = m;
+  }
+}
+
+// Weights of 32 keys against the maximum as it stands, and their sum.
+template <typename T> __device__ inline float weigh(const f32x16& s, float c, float minus_m, Weights<T>& w) {
+  float a = 0.f, b = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; r += 2) {
+    const float x = exp_diff<T>(s[r], c, minus_m), y = exp_diff<T>(s[r + 1], c, minus_m);
+    w.set(r, x, y);
+    if (r & 2) b += x + y;
+    else a += x + y;
+  }
+  return a + b;
+}
+
+// The maximum is taken anew only where a sum of weights against the old one nears overflow (and on a wave's first tile, whose
+// old maximum is -inf): fp32 and bf16 share their exponents, so a stale maximum costs no digits.
+constexpr float kStaleLimit = 0x1p60f;
+
+template <typename T, int D, int MOD>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel(Masked p, Plan plan) {
+  using G = Geo<T, D>;
+  constexpr int TILEB = G::TILEB, NDT = G::NDT;
+  __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * TILEB];      // K0 | K1 | V0 | V1
+  __shared__ int span_s[4][4];
+  __shared__ unsigned bad[2];
+
+  const int item = item_of_xcd(plan.per_xcd);
+  if ((int)(blockIdx.x / 8) >= plan.per_xcd || item >= plan.total) return;
+  const int part = item % plan.n_parts, unit = item / plan.n_parts;
+  const int bh = unit / plan.n_qt, b = bh / p.heads, head = bh % p.heads;
+  const int qt = p.causal ? plan.n_qt - 1 - unit % plan.n_qt : unit % plan.n_qt;     // the tiles with most keys first
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lam = lane & 31, h = lane >> 5;
+
+  const int row = qt * kQRows + 32 * wave + lam;
+  Interval iv{0, 0};
+  if (row < p.q_len) iv = keys_of_row(p, b, row);
+  const bool sees = iv.lo < iv.hi;
+  const Span ws = span_of_wave(iv);
+  if (lane == 0) {
+    span_s[wave][0] = ws.lo;
+    span_s[wave][1] = ws.hi;
+    span_s[wave][2] = ws.full_lo;
+    span_s[wave][3] = ws.full_hi;
+  }
+  if (tid < 2) bad[tid] = 0u;
+
+  const unsigned char* kg = p.k + b * p.sk.batch + (head / p.group) * p.sk.head;
+  const unsigned char* vg = p.v + b * p.sv.batch + (head / p.group) * p.sv.head;
+  const unsigned lds = (unsigned)(unsigned long long)(LDS_PTR(unsigned char)) & stage[0];
+  Loader<T, D> lk, lv;
+  lk.init(wave, lane, (unsigned)p.sk.token);
+  lv.init(wave, lane, (unsigned)p.sv.token);
+  Reader<T, D> rd;
+  rd.init(lane, lds);
+
+  u32x4 q[G::STEPS];                             // rows that see nothing take part as rows of zeros
+  {
+    const unsigned char* src = p.q + b * p.sq.batch + head * p.sq.head + (long long)row * p.sq.token;
+#pragma unroll
+    for (int s = 0; s < G::STEPS; ++s) {
+      q[s] = u32x4{0, 0, 0, 0};
+      if (sees) q[s] = *reinterpret_cast<const u32x4*>(src + 32 * s + 16 * h);
+    }
+  }
+  // Scores: raw products times c, or, capped or biased, made final in place and c = 1.  The log2 domain in bf16.
+  const float unit_scale = sizeof(T) == 2 ? kLog2e : 1.f;
+  const float c = MOD ? 1.f : p.scale * unit_scale;
+  const float to_cap = MOD & CAP ? p.scale / p.cap : p.scale * unit_scale, cap = p.cap * unit_scale;
+  const float slope = MOD & BIAS ? p.slopes[head] * unit_scale : 0.f;
+  const int pos = row + p.kv_len - p.q_len;
+
+  Row<T, D> st;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt) st.o[dt] = (f32x16){0};
+  st.m = -INFINITY;
+  st.l = 0.f;
+
+  __syncthreads();
+  Span gs{span_s[0][0], span_s[0][1], span_s[0][2], span_s[0][3]};
+#pragma unroll
+  for (int w = 1; w < 4; ++w) gs = join(gs, Span{span_s[w][0], span_s[w][1], span_s[w][2], span_s[w][3]});
+  gs = Span{__builtin_amdgcn_readfirstlane(gs.lo), __builtin_amdgcn_readfirstlane(gs.hi), __builtin_amdgcn_readfirstlane(gs.full_lo),
+            __builtin_amdgcn_readfirstlane(gs.full_hi)};
+  int t_begin = 0, t_end = 0;
+  if (gs.lo < gs.hi) {
+    t_begin = gs.lo / kRows;
+    t_end = (gs.hi + kRows - 1) / kRows;
+  }
+  if (plan.n_parts > 1) {
+    const int n = t_end - t_begin, first = t_begin;
+    t_begin = first + (int)((long long)n * part / plan.n_parts);
+    t_end = first + (int)((long long)n * (part + 1) / plan.n_parts);
+  }
+
+  auto load_k = [&](int t, int stage_at) {
+    lk.load(wave, lane, kg + (long long)t * kRows * p.sk.token, p.kv_len - t * kRows, lds + stage_at * TILEB);
+  };
+  auto load_v = [&](int t, int stage_at) {
+    lv.load(wave, lane, vg + (long long)t * kRows * p.sv.token, p.kv_len - t * kRows, lds + (2 + stage_at) * TILEB);
+  };
+  f32x16 s0, s1;                                 // S^T of the tile at hand: keys 0..31, 32..63
+  auto scores = [&](int t, unsigned off) {
+    if (!touches(ws, t * kRows, kRows)) return;
+    s0 = rows_times<T, D, 0>(rd, off, q);
+    s1 = rows_times<T, D, 32>(rd, off, q);
+    if (MOD) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = t * kRows + (r / 4) * 8 + 4 * h + r % 4;
+        float x = s0[r] * to_cap, y = s1[r] * to_cap;
+        if (MOD & CAP) {
+          x = cap * tanh_of<T>(x);
+          y = cap * tanh_of<T>(y);
+        }
+        if (MOD & BIAS) {
+          x = fmaf(-slope, fabsf((float)(pos - key)), x);
+          y = fmaf(-slope, fabsf((float)(pos - key - 32)), y);
+        }
+        s0[r] = x;
+        s1[r] = y;
+      }
+    }
+  };
+
+  if (t_begin < t_end) {
+    load_k(t_begin, 0);
+    wait_loads();
+    __syncthreads();
+    if (t_begin + 1 < t_end) load_k(t_begin + 1, 1);
+    load_v(t_begin, 0);
+    scores(t_begin, 0);
+  }
+  for (int t = t_begin; t < t_end; ++t) {
+    const int par = (t - t_begin) & 1;
+    const unsigned v_off = (2 + par) * TILEB;
+    wait_loads();
+    __syncthreads();
+    if (t + 2 < t_end) load_k(t + 2, par);
+    if (t + 1 < t_end) load_v(t + 1, par ^ 1);
+    unsigned bad0 = 0u, bad1 = 0u;
+    if (!covers(gs, t * kRows, kRows)) {         // seen in part by some row of the workgroup
+      clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0] + v_off, (LDS_PTR(unsigned))&bad[0], tid);
+      __syncthreads();
+      bad0 = __builtin_amdgcn_readfirstlane(bad[0]);
+      bad1 = __builtin_amdgcn_readfirstlane(bad[1]);
+      if (bad0 | bad1) {
+        __syncthreads();
+        if (tid < 2) bad[tid] = 0u;
+      }
+    }
+    if (touches(ws, t * kRows, kRows)) {
+      if (!covers(ws, t * kRows, kRows)) {
+        const unsigned n = (unsigned)(iv.hi - iv.lo);
+        const int at = t * kRows + 4 * h - iv.lo;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = (r / 4) * 8 + r % 4;
+          if ((unsigned)(at + key) >= n) s0[r] = -INFINITY;
+          if ((unsigned)(at + key + 32) >= n) s1[r] = -INFINITY;
+        }
+      }
+      Weights<T> w0, w1;
+      float sum = weigh<T>(s0, c, -st.m, w0) + weigh<T>(s1, c, -st.m, w1);
+      if (__builtin_expect(__any(!(sum < kStaleLimit)), 0)) {
+        // Row by row, so that what a row gives does not hang on its neighbours.  The products are rounded as the maximum is
+        // taken of them: the largest key has weight 1, whatever its size.
+        bool again = !(sum < kStaleLimit);
+        again |= (bool)__shfl_xor((int)again, 32);
+        const float f = again ? c : 1.f, c2 = again ? 1.f : c;
+        {
+#pragma clang fp contract(off)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            s0[r] *= f;
+            s1[r] *= f;
+          }
+        }
+        raise_max<T, D>(st, again ? fmaxf(max_of(s0), max_of(s1)) : -INFINITY);
+        const float nm = st.m == -INFINITY ? 0.f : -st.m;
+        sum = weigh<T>(s0, c2, nm, w0) + weigh<T>(s1, c2, nm, w1);
+      }
+      st.l += sum;
+      cols_times<T, D, 0>(rd, v_off, w0, st.o);
+      cols_times<T, D, 32>(rd, v_off, w1, st.o);
+      while (__builtin_expect((bad0 | bad1) != 0u, 0)) {      // values of inf or NaN, for the rows that see them
+        const int r = bad0 ? __builtin_ctz(bad0) : 32 + __builtin_ctz(bad1);
+        if (bad0) bad0 &= bad0 - 1u;
+        else bad1 &= bad1 - 1u;
+        const int key = t * kRows + r;
+        if (key >= p.kv_len) break;
+        const T* src = reinterpret_cast<const T*>(vg + (long long)key * p.sv.token);
+        const bool mine = key >= iv.lo && key < iv.hi;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float x = (float)src[32 * dt + (e / 4) * 8 + 4 * h + e % 4];
+            if (mine && !(fabsf(x) < INFINITY)) st.o[dt][e] += x;
+          }
+      }
+    }
+    if (t + 1 < t_end) scores(t + 1, (par ^ 1) * TILEB);
+  }
+
+  st.l += __shfl_xor(st.l, 32);
+  if (plan.n_parts > 1) {
+    float* po = plan.part_o + ((size_t)item * kQRows + 32 * wave + lam) * D;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 w = {st.o[dt][4 * g], st.o[dt][4 * g + 1], st.o[dt][4 * g + 2], st.o[dt][4 * g + 3]};
+        *reinterpret_cast<f32x4*>(po + 32 * dt + 8 * g + 4 * h) = w;
+      }
+    if (h == 0) {
+      plan.part_ml[((size_t)item * 2 + 0) * kQRows + 32 * wave + lam] = st.m;
+      plan.part_ml[((size_t)item * 2 + 1) * kQRows + 32 * wave + lam] = sees ? st.l : 0.f;
+    }
+    return;
+  }
+  if (row < p.q_len) {
+    const float inv = 1.f / st.l;
+    unsigned char* dst = p.out + b * p.so.batch + head * p.so.head + (long long)row * p.so.token;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = sees ? st.o[dt][4 * g + e] * inv : 0.f;
+        const int ch = 32 * dt + 8 * g + 4 * h;
+        if constexpr (sizeof(T) == 2)
+          *reinterpret_cast<u32x2*>(dst + 2 * ch) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+        else
+          *reinterpret_cast<f32x4*>(dst + 4 * ch) = x;
+      }
+    if (p.lse && h == 0) p.lse[(size_t)bh * p.q_len + row] = sees ? log_sum<T>(st.m, st.l) : -INFINITY;
+  }
+}
+
+// Joins the parts of 128 rows: a thread has four channels of a row.  Workgroup: (batch, head, tile) x slices of its rows.
+template <typename T, int D> __global__ __launch_bounds__(256) void masked_join_kernel(Masked p, Plan plan) {
+  constexpr int PER_ROW = D / 4, ROWS = 256 / PER_ROW;
+  const int unit = blockIdx.y, tid = threadIdx.x;
+  const int bh = unit / plan.n_qt, b = bh / p.heads, head = bh % p.heads;
+  const int qt = p.causal ? plan.n_qt - 1 - unit % plan.n_qt : unit % plan.n_qt;
+  const int r = blockIdx.x * ROWS + tid / PER_ROW, ch = 4 * (tid % PER_ROW), row = qt * kQRows + r;
+  if (row >= p.q_len) return;
+  const size_t item = (size_t)unit * plan.n_parts;
+  float m = -INFINITY, l = 0.f;
+  for (int i = 0; i < plan.n_parts; ++i) m = fmaxf(m, plan.part_ml[((item + i) * 2) * kQRows + r]);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < plan.n_parts; ++i) {
+    const float li = plan.part_ml[((item + i) * 2 + 1) * kQRows + r];
+    if (li == 0.f) continue;                     // no key of the row in this part
+    const float f = exp_of<T>(plan.part_ml[((item + i) * 2) * kQRows + r] - m);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(plan.part_o + ((item + i) * kQRows + r) * D + ch);
+    l += li * f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += x[e] * f;
+  }
+  const bool sees = l != 0.f;
+  const float inv = sees ? 1.f / l : 0.f;
+  unsigned char* dst = p.out + b * p.so.batch + head * p.so.head + (long long)row * p.so.token;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<u32x2*>(dst + 2 * ch) = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+  else
+    *reinterpret_cast<f32x4*>(dst + 4 * ch) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  if (p.lse && ch == 0) p.lse[(size_t)bh * p.q_len + row] = sees ? log_sum<T>(m, l) : -INFINITY;
+}
+
+Plan plan_of(const Masked& m) {
+  Plan pl{};
+  pl.n_qt = (m.q_len + kQRows - 1) / kQRows;
+  const long long units = (long long)m.batch * m.heads * pl.n_qt;
+  // Keys are shared out where the tiles alone leave compute units idle and there are keys enough to share.
+  const long long slots = m.dtype == PISA_BF16 ? 512 : 256;
+  const int tiles = (m.kv_len + kRows - 1) / kRows;
+  long long parts = units >= slots ? 1 : slots / units;
+  parts = parts < tiles / 4 ? parts : tiles / 4;
+  pl.n_parts = parts < 1 ? 1 : (int)parts;
+  pl.total = (int)(units * pl.n_parts);
+  pl.per_xcd = (pl.total + 7) / 8;
+  return pl;
+}
+
+template <typename T, int D> hipError_t launch_td(const Masked& m, const Plan& pl, hipStream_t stream) {
+  const dim3 grid(8 * pl.per_xcd), block(256);
+  switch ((m.cap > 0.f ? CAP : 0) | (m.slopes ? BIAS : 0)) {
+    case 0: hipLaunchKernelGGL((masked_fwd_kernel<T, D, 0>), grid, block, 0, stream, m, pl); break;
+    case CAP: hipLaunchKernelGGL((masked_fwd_kernel<T, D, CAP>), grid, block, 0, stream, m, pl); break;
+    case BIAS: hipLaunchKernelGGL((masked_fwd_kernel<T, D, BIAS>), grid, block, 0, stream, m, pl); break;
+    default: hipLaunchKernelGGL((masked_fwd_kernel<T, D, CAP | BIAS>), grid, block, 0, stream, m, pl); break;
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || pl.n_parts == 1) return e;
+  hipLaunchKernelGGL((masked_join_kernel<T, D>), dim3(kQRows / (256 / (D / 4)), pl.total / pl.n_parts), block, 0, stream, m, pl);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t masked_workspace_bytes(const Masked& m) {
+  const Plan pl = plan_of(m);
+  return pl.n_parts == 1 ? 0 : (size_t)pl.total * kQRows * (m.d + 2) * sizeof(float);
+}
+
+hipError_t launch_masked_attention(const Masked& m, hipStream_t stream) {
+  Plan pl = plan_of(m);
+  if (pl.n_parts > 1) {
+    pl.part_o = static_cast<float*>(m.workspace);
+    pl.part_ml = pl.part_o + (size_t)pl.total * kQRows * m.d;
+  }
+  if (m.dtype == PISA_BF16) return m.d == 64 ? launch_td<__bf16, 64>(m, pl, stream) : launch_td<__bf16, 128>(m, pl, stream);
+  return m.d == 64 ? launch_td<float, 64>(m, pl, stream) : launch_td<float, 128>(m, pl, stream);
+}
+
+}  // namespace pisa

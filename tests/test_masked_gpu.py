@@ -1,0 +1,295 @@
+"""pisa_masked_attention and pisa_masked_attention_backward against the fp64 oracle: types, masks that leave rows empty,
+odd sizes, strides, shared heads, non-finite values in masked places, capture into a graph."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import masked_oracle as mo
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def make(seed, b, h, kvh, n, m, d, dtype, tokens_first=False, spread=1.5):
+    g = torch.Generator().manual_seed(seed)
+
+    def one(heads, length, s=1.0):
+        shape = (b, length, heads, d) if tokens_first else (b, heads, length, d)
+        x = (s * torch.randn(shape, generator=g)).to(DT[dtype])
+        return (x.transpose(1, 2) if tokens_first else x)
+    q, k, v, dout = one(h, n, spread), one(kvh, m), one(kvh, m), one(h, n)
+    up = lambda x: x.to(DEV) if not tokens_first else x.transpose(1, 2).contiguous().to(DEV).transpose(1, 2)
+    return up(q), up(k), up(v), up(dout)
+
+
+def f64(t):
+    return t.detach().to("cpu", torch.float64).numpy()
+
+
+def ints(x):
+    return None if x is None else torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def n_terms(m, d):
+    return m + 4 * d + 64        # products of a score, weights of a row, and what the exponential adds
+
+
+def check(lib, q, k, v, dout, causal, docs, prefix, softcap=0.0, slopes=None, backward=True, **kw):
+    b, h, n, d = q.shape
+    m = k.shape[2]
+    see = mo.visible(b, n, m, causal, docs, prefix)
+    scale = lib.resolved_scale(d)
+    slo = None if slopes is None else torch.tensor(slopes, dtype=torch.float32, device=DEV)
+    args = dict(causal=causal, doc_offsets=ints(docs), prefix=ints(prefix), softcap=softcap, slopes=slo)
+    out, lse = lib.masked_attention(q, k, v, want_lse=True, **args, **kw)
+    grads = lib.masked_attention_backward(q, k, v, out, lse, dout, **args) if backward else None
+    torch.cuda.synchronize()
+    slo64 = None if slopes is None else slo.double().cpu().numpy()
+    ref = mo.attention(f64(q), f64(k), f64(v), see, scale, softcap, slo64, f64(dout) if backward else None)
+    eps = 2.0 ** -7 if q.dtype == torch.bfloat16 else 2.0 ** -23
+    terms = n_terms(m, d)
+    bound = mo.forward_bounds(ref, eps, terms)
+    diff = np.abs(f64(out) - ref["out"])
+    assert np.all(diff <= bound), f"out: {np.max(diff / bound):.2f} of the bound"
+    lse_ref, lse_got = ref["lse"], f64(lse)
+    empty = np.isneginf(lse_ref)
+    assert np.array_equal(np.isneginf(lse_got), empty)
+    assert np.all(f64(out)[empty] == 0)
+    lse_tol = 2.0 ** -24 * terms * (1 + ref["zmax"])
+    assert np.abs(lse_got[~empty] - lse_ref[~empty]).max(initial=0) <= lse_tol
+    if backward:
+        bounds = mo.gradient_bounds(ref, eps, n_terms(max(m, n * h // k.shape[1]), d), scale)
+        for name, got in zip(("dq", "dk", "dv"), grads):
+            diff = np.abs(f64(got) - ref[name])
+            assert np.all(diff <= bounds[name]), f"{name}: {np.max(diff / bounds[name]):.2f} of the bound"
+    return out, lse, grads
+
+
+# (batch, heads, kv_heads, q_len, kv_len, causal, documents, prefix)
+SHAPES = [
+    (1, 1, 1, 1, 1, False, None, None),
+    (2, 2, 1, 1, 77, True, None, None),
+    (1, 3, 3, 64, 64, True, None, None),
+    (2, 4, 2, 129, 129, True, None, [[40], [0]]),
+    (1, 2, 2, 200, 200, False, [[0, 63, 64, 64, 150]], None),                     # a document of one token, an empty one, padding
+    (2, 2, 1, 191, 191, True, [[0, 100, 191, 191], [5, 70, 70, 160]], [[10, 200, 3], [0, 4, 33]]),
+    (1, 4, 1, 65, 333, True, [[0, 130, 290, 333]], None),                         # rows are the last of the positions
+    (1, 2, 2, 90, 40, True, None, None),                                          # rows before position 0 see nothing
+    (1, 2, 1, 300, 50, False, None, None),                                        # more rows than keys
+    (1, 2, 2, 257, 511, True, None, [[300]]),
+    (1, 1, 1, 130, 130, False, [[130, 130]], None),                               # nobody sees anything
+]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(str(x) for x in s[:6]))
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp32", 128), ("fp32", 64)])
+def test_against_oracle(lib, shape, dtype, d):
+    b, h, kvh, n, m, causal, docs, prefix = shape
+    q, k, v, dout = make(1, b, h, kvh, n, m, d, dtype, tokens_first=n % 2 == 1)
+    check(lib, q, k, v, dout, causal, docs, prefix)
+
+
+@pytest.mark.parametrize("softcap,bias", [(20.0, False), (0.0, True), (5.0, True)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp32", 128), ("fp32", 64)])
+def test_scores_capped_and_biased(lib, softcap, bias, dtype, d):
+    q, k, v, dout = make(2, 1, 4, 2, 150, 211, d, dtype)
+    slopes = [0.5, 0.25, 0.03, 0.0] if bias else None
+    check(lib, q, k, v, dout, True, None, [[60]], softcap, slopes)
+    check(lib, q, k, v, dout, False, [[0, 90, 211]], None, softcap, slopes)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_zero_keys(lib, dtype):
+    q, k, v, dout = make(3, 2, 2, 1, 70, 0, 64, dtype)
+    out, lse = lib.masked_attention(q, k, v, want_lse=True)
+    dq, dk, dv = lib.masked_attention_backward(q, k, v, out, lse, dout)
+    torch.cuda.synchronize()
+    assert torch.count_nonzero(out) == 0 and torch.count_nonzero(dq) == 0
+    assert torch.isneginf(lse).all()
+    assert dk.shape == k.shape and dv.shape == v.shape
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp32", 64)])
+def test_few_rows_and_many_keys_are_shared_out(lib, dtype, d):
+    q, k, v, dout = make(4, 1, 2, 1, 3, 2500, d, dtype)
+    shape = lib._masked_shape(q, k, v, q, True, None, 0.0, None)
+    assert lib.raw().pisa_masked_attention_workspace_bytes(shape) > 0
+    check(lib, q, k, v, dout, True, None, None)
+    check(lib, q, k, v, dout, True, [[0, 2499, 2500]], None)      # rows that see one key, in the last part alone
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp32", 128)])
+def test_what_is_masked_may_be_anything(lib, dtype, d):
+    docs = [[0, 70, 90, 170]]
+    n = 200
+    q, k, v, dout = make(5, 1, 2, 2, n, n, d, dtype)
+    for causal in (False, True):
+        ref = check(lib, q, k, v, dout, causal, docs, None)
+        q2, k2, v2, g2 = (x.clone() for x in (q, k, v, dout))
+        for i, x in enumerate((q2, k2, v2, g2)):                   # padding behind the last document
+            x[:, :, 170::3] = float("nan")
+            x[:, :, 171::3] = float("inf")
+            x[:, :, 172::3] = -torch.finfo(x.dtype).max
+        args = dict(causal=causal, doc_offsets=ints(docs))
+        out, lse = lib.masked_attention(q2, k2, v2, want_lse=True, **args)
+        grads = lib.masked_attention_backward(q2, k2, v2, out, lse, g2, **args)
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1])
+        for a, r in zip(grads, ref[2]):
+            assert torch.equal(a, r)
+        # a broken document leaves the others alone, in tiles that they share
+        q3, k3, v3, g3 = (x.clone() for x in (q, k, v, dout))
+        for x in (q3, k3, v3, g3):
+            x[:, :, 75] = float("nan")
+            x[:, :, 80] = float("inf")
+        out, lse = lib.masked_attention(q3, k3, v3, want_lse=True, **args)
+        grads = lib.masked_attention_backward(q3, k3, v3, out, lse, g3, **args)
+        torch.cuda.synchronize()
+        others = [i for i in range(n) if not 70 <= i < 90]
+        assert torch.equal(out[:, :, others], ref[0][:, :, others]) and torch.equal(lse[:, :, others], ref[1][:, :, others])
+        for a, r in zip(grads, ref[2]):
+            assert torch.equal(a[:, :, others], r[:, :, others])
+        assert not torch.isfinite(out[:, :, 80:90]).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_value_of_infinity_reaches_the_rows_that_see_it(lib, dtype):
+    q, k, v, dout = make(6, 1, 1, 1, 100, 100, 64, dtype)
+    ref, _ = lib.masked_attention(q, k, v, causal=True)
+    v2 = v.clone()
+    v2[0, 0, 60, 3] = float("inf")
+    v2[0, 0, 61, 40] = float("nan")
+    out, _ = lib.masked_attention(q, k, v2, causal=True)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:, :, :60], ref[:, :, :60])
+    assert torch.isposinf(out[0, 0, 60:, 3]).all() and torch.isnan(out[0, 0, 61:, 40]).all()
+    rest = [c for c in range(64) if c not in (3, 40)]
+    assert torch.equal(out[0, 0, 60:][:, rest], ref[0, 0, 60:][:, rest])
+
+
+def test_scores_of_any_size(lib):
+    """Runaway maxima (each tile's scores above the last one's), and scores far below 0."""
+    q, k, v, dout = make(7, 1, 2, 2, 300, 300, 128, "bf16")
+    ramp = torch.linspace(0.1, 40.0, 300, device=DEV)[None, None, :, None]
+    check(lib, q, (k.float() * ramp).to(k.dtype), v, dout, True, None, None, backward=False)
+    check(lib, q, (k.float() * ramp.flip(2)).to(k.dtype), v, dout, False, None, None, backward=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_packed_projections_and_broadcast_keys(lib, dtype):
+    """q, k, v as views of one [batch, tokens, 3, heads, d] tensor; gradients into views of another; a k shared by the batch."""
+    d, n, h = 64, 140, 2
+    g = torch.Generator().manual_seed(8)
+    qkv = torch.randn(2, n, 3, h, d, generator=g).to(DT[dtype]).to(DEV)
+    q, k, v = (qkv[:, :, i].transpose(1, 2) for i in range(3))
+    dout = torch.randn(2, n, h, d, generator=g).to(DT[dtype]).to(DEV).transpose(1, 2)
+    ref = check(lib, q, k, v, dout, True, None, None)
+    grad = torch.full_like(qkv, 7.0)
+    spare = torch.full((2, n, h + 1, d), 7.0, dtype=DT[dtype], device=DEV)
+    out = spare[:, :, :h].transpose(1, 2)
+    lib.masked_attention(q, k, v, causal=True, out=out)
+    views = [grad[:, :, i].transpose(1, 2) for i in range(3)]
+    lib.masked_attention_backward(q, k, v, ref[0], ref[1], dout, causal=True, dq=views[0], dk=views[1], dv=views[2])
+    torch.cuda.synchronize()
+    assert torch.equal(out, ref[0]) and (spare[:, :, h] == 7.0).all()
+    for a, r in zip(views, ref[2]):
+        assert torch.equal(a, r)
+    one = k[:1].expand(2, h, n, d)
+    check(lib, q, one, v, dout, True, None, None, backward=False)
+
+
+def test_equal_calls_give_equal_bits(lib):
+    q, k, v, dout = make(9, 1, 8, 2, 700, 700, 128, "bf16")
+    runs = []
+    for _ in range(3):
+        out, lse = lib.masked_attention(q, k, v, causal=True, want_lse=True)
+        runs.append((out, lse) + lib.masked_attention_backward(q, k, v, out, lse, dout, causal=True))
+    torch.cuda.synchronize()
+    for r in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(r, runs[0]))
+
+
+@pytest.mark.parametrize("softcap,bias", [(0.0, False), (4.0, True)])
+def test_gradients_against_differences(lib, softcap, bias):
+    """Central differences of the oracle's forward pass along random directions, fp32 kernels."""
+    d, n = 64, 75
+    q, k, v, dout = make(10, 1, 2, 1, n, n, d, "fp32", spread=1.0)
+    slopes = np.array([0.1, 0.02]) if bias else None
+    docs, prefix = [[0, 40, 70]], [[9, 0]]
+    slo = None if slopes is None else torch.tensor(slopes, dtype=torch.float32, device=DEV)
+    args = dict(causal=True, doc_offsets=ints(docs), prefix=ints(prefix), softcap=softcap, slopes=slo)
+    out, lse = lib.masked_attention(q, k, v, want_lse=True, **args)
+    grads = [f64(x) for x in lib.masked_attention_backward(q, k, v, out, lse, dout, **args)]
+    torch.cuda.synchronize()
+    see, scale = mo.visible(1, n, n, True, docs, prefix), lib.resolved_scale(d)
+    base, G = [f64(x) for x in (q, k, v)], f64(dout)
+    slo64 = None if slopes is None else slo.double().cpu().numpy()
+    loss = lambda x: float((mo.attention(*x, see, scale, softcap, slo64)["out"] * G).sum())
+    rng = np.random.default_rng(0)
+    for which in range(3):
+        for _ in range(3):
+            u = rng.standard_normal(base[which].shape)
+            step = 1e-4 / np.sqrt(u.size)
+            plus, minus = ([x + (s * step * u if i == which else 0) for i, x in enumerate(base)] for s in (1, -1))
+            diff = (loss(plus) - loss(minus)) / (2 * step)
+            # fp32 sums of some thousand terms (2^-24 each); the differences' own error is of third order in the step
+            tol = 2.0 ** -24 * 2000 * float((np.abs(grads[which]) * np.abs(u)).sum()) + 1e-6 * abs(diff)
+            assert abs(diff - float((grads[which] * u).sum())) <= tol
+
+
+def test_graph_replays_match_eager_calls(lib):
+    q, k, v, dout = make(11, 1, 4, 2, 333, 333, 128, "bf16")
+    docs = ints([[0, 200, 320]])
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device=DEV)
+    dq, dk, dv = (torch.empty_like(x) for x in (q, k, v))
+    shape = lib._masked_shape(q, k, v, out, True, docs, 0.0, None)
+    ws = torch.empty(max(lib.raw().pisa_masked_attention_workspace_bytes(shape),
+                         lib.raw().pisa_masked_attention_backward_workspace_bytes(shape)), dtype=torch.uint8, device=DEV)
+
+    def step():
+        lib.masked_attention(q, k, v, causal=True, doc_offsets=docs, out=out, lse=lse, workspace=ws)
+        lib.masked_attention_backward(q, k, v, out, lse, dout, causal=True, doc_offsets=docs, dq=dq, dk=dk, dv=dv, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (20, 21, 22):
+        for dst, src in zip((q, k, v, dout), make(seed, 1, 4, 2, 333, 333, 128, "bf16")):
+            dst.copy_(src)
+        step()
+        torch.cuda.synchronize()
+        eager = [x.clone() for x in (out, lse, dq, dk, dv)]
+        for x in (out, lse, dq, dk, dv):
+            x.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((out, lse, dq, dk, dv), eager))
+
+
+def test_on_a_stream_of_its_own(lib):
+    q, k, v, _ = make(12, 1, 4, 4, 500, 500, 128, "bf16")
+    ref, _ = lib.masked_attention(q, k, v, causal=True)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        out, _ = lib.masked_attention(q, k, v, causal=True)
+    side.synchronize()
+    assert torch.equal(out, ref)
+
+
+def test_without_masks_as_dense_attention(lib):
+    """The same function as dense_attention where nothing is masked (other kernels: bf16 weights rounded against other maxima)."""
+    q, k, v, _ = make(13, 1, 3, 3, 700, 700, 128, "bf16")
+    a, la = lib.masked_attention(q, k, v, want_lse=True)
+    b, lb = lib.dense_attention(q, k, v, want_lse=True)
+    torch.cuda.synchronize()
+    ref = mo.attention(f64(q), f64(k), f64(v), mo.visible(1, 700, 700), lib.resolved_scale(128))
+    bound = 2 * mo.forward_bounds(ref, 2.0 ** -7, n_terms(700, 128))
+    assert np.all(np.abs(f64(a) - f64(b)) <= bound)
+    assert (la - lb).abs().max() <= 2 * 2.0 ** -24 * n_terms(700, 128) * (1 + ref["zmax"])
