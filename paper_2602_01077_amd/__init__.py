@@ -8,6 +8,7 @@ paper_2602_01077_amd.build`); there is no fallback path of any kind.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from typing import Optional, Tuple
@@ -179,8 +180,10 @@ def _dev(t: Optional[torch.Tensor], name: str, dtype=None, like: Optional[torch.
     return ctypes.c_void_p(t.data_ptr())
 
 
-def _stream() -> ctypes.c_void_p:
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+def _stream() -> int:
+    """The current stream's handle.  Straight from the runtime's own table: a torch.cuda.Stream object costs 4 us a call, a
+    third of what a short call takes on the host."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def workspace_bytes(shape: PisaShape) -> int:
@@ -306,22 +309,15 @@ def dense_attention(q, k, v, block: int = 64, scale: Optional[float] = None,
     return out, lse
 
 
-def _strides(t: torch.Tensor, name: str) -> PisaStrides:
-    """Of a [batch, heads, tokens, head_dim] view; the channels of a row have to lie together."""
-    b, h, n, c = t.stride()
-    if c != 1 and t.shape[3] > 1:
-        raise ValueError(f"{name}: the last dimension must be contiguous")
-    return PisaStrides(b, h, n if t.shape[2] > 1 else max(n, t.shape[3]))
-
-
-def _same_device(ref: torch.Tensor, **others: Optional[torch.Tensor]) -> None:
-    if not ref.is_cuda:
+def _on_current_device(ref: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    device = ref.get_device()
+    if device < 0:
         raise ValueError("tensors must live on the GPU")
-    if ref.device.index != torch.cuda.current_device():
+    if device != torch._C._cuda_getDevice():
         raise ValueError(f"tensors live on {ref.device}, the current device is cuda:{torch.cuda.current_device()}")
-    for name, t in others.items():
-        if t is not None and t.device != ref.device:
-            raise ValueError(f"{name} lives on {t.device}, q on {ref.device}")
+    for t in others:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"all tensors must live on {ref.device}, got one on {t.device}")
 
 
 def _plain(t: Optional[torch.Tensor], name: str, dtype, shape) -> Optional[int]:
@@ -330,46 +326,65 @@ def _plain(t: Optional[torch.Tensor], name: str, dtype, shape) -> Optional[int]:
         return None
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _workspace(t: Optional[torch.Tensor], need: int, device) -> Tuple[Optional[torch.Tensor], int]:
+def _workspace(t: Optional[torch.Tensor], need: int, device) -> Tuple[Optional[torch.Tensor], Optional[int], int]:
+    """(the tensor, which has to live until the launch, its address, its size)"""
     if t is None:
-        t = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-        return t, need
+        if not need:
+            return None, None, 0
+        t = torch.empty(need, dtype=torch.uint8, device=device)
+        return t, t.data_ptr(), need
     if not t.is_contiguous() or t.device != device:
         raise ValueError("workspace must be contiguous and on the tensors' device")
-    return t, t.numel() * t.element_size()
+    return t, t.data_ptr(), t.numel() * t.element_size()
 
 
-def _masked_shape(q, k, v, out, causal, doc_offsets, softcap, scale) -> PisaMaskedShape:
-    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+def _strides(size, stride, name: str) -> PisaStrides:
+    """Of a [batch, heads, tokens, head_dim] view; the channels of a row have to lie together."""
+    if stride[3] != 1 and size[3] > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return PisaStrides(stride[0], stride[1], stride[2] if size[2] > 1 else max(stride[2], size[3]))
+
+
+# The structures of recent calls, by sizes, strides and options (building one anew costs as much as the launch).
+@functools.lru_cache(maxsize=1024)
+def _masked_plan(q_size, k_size, v_size, out_size, q_stride, k_stride, v_stride, out_stride, dtype, causal, docs, softcap, scale):
+    """(shape, workspace of the forward call, of the backward call)"""
+    if len(q_size) != 4 or len(k_size) != 4 or len(v_size) != 4:
         raise ValueError("expected q, k, v of shape [batch, heads, tokens, head_dim]")
-    b, h, n, d = q.shape
-    if k.shape != v.shape or k.shape[0] != b or k.shape[3] != d:
-        raise ValueError(f"k and v must be alike and match q in batch and head_dim: {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)}")
-    if k.dtype != q.dtype or v.dtype != q.dtype:
-        raise TypeError("q, k and v must have one dtype")
-    if out.shape != q.shape or out.dtype != q.dtype:
-        raise ValueError("out must match q in shape and dtype")
+    b, h, n, d = q_size
+    if k_size != v_size or k_size[0] != b or k_size[3] != d:
+        raise ValueError(f"k and v must be alike and match q in batch and head_dim: {tuple(q_size)}, {tuple(k_size)}, {tuple(v_size)}")
+    if out_size != q_size:
+        raise ValueError("out must match q in shape")
+    shape = PisaMaskedShape(b, h, k_size[1], n, k_size[2], d, dtype, 1 if causal else 0, docs, scale, softcap,
+                            _strides(q_size, q_stride, "q"), _strides(k_size, k_stride, "k"), _strides(v_size, v_stride, "v"),
+                            _strides(out_size, out_stride, "out"))
+    return shape, _lib.pisa_masked_attention_workspace_bytes(shape), _lib.pisa_masked_attention_backward_workspace_bytes(shape)
+
+
+def _masked_call(q, k, v, out, causal, doc_offsets, softcap, scale):
+    if k.dtype != q.dtype or v.dtype != q.dtype or out.dtype != q.dtype:
+        raise TypeError("q, k, v and out must have one dtype")
     docs = 0
     if doc_offsets is not None:
         if doc_offsets.dim() != 2 or doc_offsets.shape[1] < 2:
             raise ValueError("doc_offsets must have shape [batch, documents + 1], with one document at least")
         docs = doc_offsets.shape[1] - 1
-    return PisaMaskedShape(b, h, k.shape[1], n, k.shape[2], d, _dtype_code(q), 1 if causal else 0, docs,
-                           0.0 if scale is None else float(scale), float(softcap),
-                           _strides(q, "q"), _strides(k, "k"), _strides(v, "v"), _strides(out, "out"))
+    return _masked_plan(q.shape, k.shape, v.shape, out.shape, q.stride(), k.stride(), v.stride(), out.stride(), _dtype_code(q),
+                        bool(causal), docs, float(softcap), 0.0 if scale is None else float(scale))
 
 
-def _mask_pointers(shape: PisaMaskedShape, doc_offsets, prefix, slopes):
-    return (_plain(doc_offsets, "doc_offsets", torch.int32, (shape.batch, shape.num_docs + 1)),
-            _plain(prefix, "prefix", torch.int32, (shape.batch, max(shape.num_docs, 1))),
-            _plain(slopes, "slopes", torch.float32, (shape.heads,)))
+def masked_attention_workspace_bytes(q, k, v, causal: bool = False, doc_offsets: Optional[torch.Tensor] = None,
+                                     backward: bool = False) -> int:
+    """Bytes of workspace that masked_attention, or masked_attention_backward, needs for tensors of these shapes."""
+    return _masked_call(q, k, v, q, causal, doc_offsets, 0.0, None)[2 if backward else 1]
 
 
 def masked_attention(q, k, v, causal: bool = False, doc_offsets: Optional[torch.Tensor] = None,
@@ -383,15 +398,17 @@ def masked_attention(q, k, v, causal: bool = False, doc_offsets: Optional[torch.
     `out` is laid out as q unless given."""
     if out is None:
         out = torch.empty_like(q)
-    shape = _masked_shape(q, k, v, out, causal, doc_offsets, softcap, scale)
+    shape, need, _ = _masked_call(q, k, v, out, causal, doc_offsets, softcap, scale)
     if lse is None and want_lse:
         lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
-    _same_device(q, k=k, v=v, out=out, lse=lse, doc_offsets=doc_offsets, prefix=prefix, slopes=slopes)
-    docs, pre, slo = _mask_pointers(shape, doc_offsets, prefix, slopes)
-    workspace, size = _workspace(workspace, _lib.pisa_masked_attention_workspace_bytes(shape), q.device)
-    _check(_lib.pisa_masked_attention(shape, q.data_ptr(), k.data_ptr(), v.data_ptr(), docs, pre, slo, out.data_ptr(),
-                                      _plain(lse, "lse", torch.float32, q.shape[:3]),
-                                      None if workspace is None else workspace.data_ptr(), size, _stream()))
+    _on_current_device(q, k, v, out, lse, doc_offsets, prefix, slopes)
+    keep, ws, size = _workspace(workspace, need, q.device)
+    _check(_lib.pisa_masked_attention(
+        shape, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        _plain(doc_offsets, "doc_offsets", torch.int32, (shape.batch, shape.num_docs + 1)),
+        _plain(prefix, "prefix", torch.int32, (shape.batch, shape.num_docs or 1)),
+        _plain(slopes, "slopes", torch.float32, (shape.heads,)),
+        out.data_ptr(), _plain(lse, "lse", torch.float32, q.shape[:3]), ws, size, _stream()))
     return out, lse
 
 
@@ -403,57 +420,66 @@ def masked_attention_backward(q, k, v, out, lse, dout, causal: bool = False, doc
     """pisa_masked_attention_backward: gradients of masked_attention(...) with the same arguments, from its out and lse and
     the gradient dout of out.  Returns (dq, dk, dv)."""
     dq, dk, dv = (torch.empty_like(x) if g is None else g for x, g in ((q, dq), (k, dk), (v, dv)))
-    shape = _masked_shape(q, k, v, out, causal, doc_offsets, softcap, scale)
+    shape, _, need = _masked_call(q, k, v, out, causal, doc_offsets, softcap, scale)
     for name, t, like in (("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
         if t.shape != like.shape or t.dtype != like.dtype:
             raise ValueError(f"{name} must have shape {tuple(like.shape)} and dtype {like.dtype}")
-    strides = PisaGradStrides(_strides(dout, "dout"), _strides(dq, "dq"), _strides(dk, "dk"), _strides(dv, "dv"))
-    _same_device(q, k=k, v=v, out=out, lse=lse, dout=dout, doc_offsets=doc_offsets, prefix=prefix, slopes=slopes, dq=dq, dk=dk,
-                 dv=dv)
-    docs, pre, slo = _mask_pointers(shape, doc_offsets, prefix, slopes)
-    workspace, size = _workspace(workspace, _lib.pisa_masked_attention_backward_workspace_bytes(shape), q.device)
+    strides = PisaGradStrides(*(_strides(t.shape, t.stride(), name) for name, t in
+                                (("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv))))
+    _on_current_device(q, k, v, out, lse, dout, doc_offsets, prefix, slopes, dq, dk, dv)
+    keep, ws, size = _workspace(workspace, need, q.device)
     _check(_lib.pisa_masked_attention_backward(
         shape, strides, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _plain(lse, "lse", torch.float32, q.shape[:3]),
-        dout.data_ptr(), docs, pre, slo, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-        None if workspace is None else workspace.data_ptr(), size, _stream()))
+        dout.data_ptr(), _plain(doc_offsets, "doc_offsets", torch.int32, (shape.batch, shape.num_docs + 1)),
+        _plain(prefix, "prefix", torch.int32, (shape.batch, shape.num_docs or 1)),
+        _plain(slopes, "slopes", torch.float32, (shape.heads,)),
+        dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws, size, _stream()))
     return dq, dk, dv
 
 
-def _page_strides(t: torch.Tensor, name: str) -> PisaStrides:
-    """Of a [pages, page_size, kv_heads, head_dim] view."""
-    p, n, h, c = t.stride()
-    if c != 1 and t.shape[3] > 1:
-        raise ValueError(f"{name}: the last dimension must be contiguous")
-    return PisaStrides(p, h, n if t.shape[1] > 1 else max(n, t.shape[3]))
-
-
-def _paged_shape(k_pages, v_pages, page_table, heads, softcap, scale) -> PisaPagedShape:
-    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape:
+@functools.lru_cache(maxsize=1024)
+def _paged_plan(k_size, v_size, k_stride, v_stride, dtype, table_size, heads, softcap, scale):
+    """(shape, workspace of paged_attention)"""
+    if len(k_size) != 4 or k_size != v_size:
         raise ValueError("expected k_pages and v_pages of one shape [pages, page_size, kv_heads, head_dim]")
+    if len(table_size) != 2:
+        raise ValueError("page_table must have shape [sequences, pages of the longest]")
+    pages, page, kvh, d = k_size
+
+    def strides(st, name):                 # as [pages, kv_heads, page_size, head_dim], the order of PisaStrides
+        return _strides((pages, kvh, page, d), (st[0], st[2], st[1], st[3]), name)
+    shape = PisaPagedShape(table_size[0], heads if heads else kvh, kvh, d, dtype, page, pages, table_size[1], scale, softcap,
+                           strides(k_stride, "k_pages"), strides(v_stride, "v_pages"))
+    return shape, _lib.pisa_paged_attention_workspace_bytes(shape)
+
+
+def _paged_call(k_pages, v_pages, page_table, heads, softcap, scale):
     if v_pages.dtype != k_pages.dtype:
         raise TypeError("k_pages and v_pages must have one dtype")
-    if page_table.dim() != 2:
-        raise ValueError("page_table must have shape [sequences, pages of the longest]")
-    n, page, kvh, d = k_pages.shape
-    return PisaPagedShape(page_table.shape[0], heads, kvh, d, _dtype_code(k_pages), page, n, page_table.shape[1],
-                          0.0 if scale is None else float(scale), float(softcap),
-                          _page_strides(k_pages, "k_pages"), _page_strides(v_pages, "v_pages"))
+    return _paged_plan(k_pages.shape, v_pages.shape, k_pages.stride(), v_pages.stride(), _dtype_code(k_pages), page_table.shape,
+                       heads, float(softcap), 0.0 if scale is None else float(scale))
 
 
 def paged_append(k, v, offsets, k_pages, v_pages, page_table, lengths) -> None:
     """pisa_paged_append: rows offsets[s] .. offsets[s+1]-1 of k and v [tokens, kv_heads, d] become the last cached tokens of
     sequence s, whose lengths[s] counts them already.  offsets int32 [sequences + 1], page_table int32 [sequences, pages],
     lengths int32 [sequences]; k_pages and v_pages as for paged_attention, written in place."""
-    shape = _paged_shape(k_pages, v_pages, page_table, k_pages.shape[2] if k_pages.dim() == 4 else 0, 0.0, None)
-    _same_device(k_pages, v_pages=v_pages, k=k, v=v, offsets=offsets, page_table=page_table, lengths=lengths)
+    shape, _ = _paged_call(k_pages, v_pages, page_table, 0, 0.0, None)
     if k.dim() != 3:
         raise ValueError("expected k and v of shape [tokens, kv_heads, head_dim]")
-    rows = (k.shape[0], shape.kv_heads, shape.head_dim)
+    _on_current_device(k_pages, v_pages, k, v, offsets, page_table, lengths)
+    tokens = k.shape[0]
+    rows = (tokens, shape.kv_heads, shape.head_dim)
     _check(_lib.pisa_paged_append(
-        shape, _plain(k, "k", k_pages.dtype, rows), _plain(v, "v", k_pages.dtype, rows), k.shape[0],
+        shape, _plain(k, "k", k_pages.dtype, rows), _plain(v, "v", k_pages.dtype, rows), tokens,
         _plain(offsets, "offsets", torch.int32, (shape.seqs + 1,)), k_pages.data_ptr(), v_pages.data_ptr(),
         _plain(page_table, "page_table", torch.int32, page_table.shape),
         _plain(lengths, "lengths", torch.int32, (shape.seqs,)), _stream()))
+
+
+def paged_attention_workspace_bytes(q, k_pages, v_pages, page_table) -> int:
+    """Bytes of workspace that paged_attention needs for tensors of these shapes (whatever the lengths)."""
+    return _paged_call(k_pages, v_pages, page_table, q.shape[1], 0.0, None)[1]
 
 
 def paged_attention(q, k_pages, v_pages, page_table, lengths, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,
@@ -461,24 +487,25 @@ def paged_attention(q, k_pages, v_pages, page_table, lengths, softcap: float = 0
                     lse: Optional[torch.Tensor] = None, want_lse: bool = False,
                     workspace: Optional[torch.Tensor] = None):
     """pisa_paged_attention: one query row per sequence and head, q [sequences, heads, d], over a cache k_pages, v_pages
-    [pages, page_size, kv_heads, d] (any strides with whole rows of channels).  Returns (out, lse or None)."""
+    [pages, page_size, kv_heads, d] (any strides with whole rows of channels; lengths int32 [sequences], page_table int32
+    [sequences, pages]).  Returns (out, lse or None)."""
     if q.dim() != 3:
         raise ValueError("expected q of shape [sequences, heads, head_dim]")
     if q.dtype != k_pages.dtype:
         raise TypeError("q and the pages must have one dtype")
-    shape = _paged_shape(k_pages, v_pages, page_table, q.shape[1], softcap, scale)
+    shape, need = _paged_call(k_pages, v_pages, page_table, q.shape[1], softcap, scale)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     if lse is None and want_lse:
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    _same_device(q, k_pages=k_pages, v_pages=v_pages, page_table=page_table, lengths=lengths, slopes=slopes, out=out, lse=lse)
+    _on_current_device(q, k_pages, v_pages, page_table, lengths, slopes, out, lse)
     rows = (shape.seqs, shape.heads, shape.head_dim)
-    workspace, size = _workspace(workspace, _lib.pisa_paged_attention_workspace_bytes(shape), q.device)
+    keep, ws, size = _workspace(workspace, need, q.device)
     _check(_lib.pisa_paged_attention(
         shape, _plain(q, "q", q.dtype, rows), k_pages.data_ptr(), v_pages.data_ptr(),
         _plain(page_table, "page_table", torch.int32, page_table.shape), _plain(lengths, "lengths", torch.int32, (shape.seqs,)),
         _plain(slopes, "slopes", torch.float32, (shape.heads,)), _plain(out, "out", q.dtype, rows),
-        _plain(lse, "lse", torch.float32, q.shape[:2]), None if workspace is None else workspace.data_ptr(), size, _stream()))
+        _plain(lse, "lse", torch.float32, rows[:2]), ws, size, _stream()))
     return out, lse
 
 

@@ -18,14 +18,19 @@ namespace {
 
 constexpr int kOwn = 128;                // rows (keys) of a workgroup, 32 to a wave
 constexpr int CAP = 1, BIAS = 2;         // bits of MOD
+constexpr float kHeavy = 0.25f;        // see masked_dq_kernel
+constexpr int kHeavyBits = 12;           // of a walk's tiles, 4 096 are told apart
 
 struct Plan {
-  int n_tiles;         // tiles of 128 rows (dq) or keys (dk, dv) to a head
-  int n_parts;         // dk, dv: workgroups that share the rows of a key tile
-  int total, per_xcd;
-  float* delta;        // [batch][heads][q_len]
-  float* part;         // n_parts > 1: [item][dk, dv][128][d]
+  Deal deal;           // of tiles of 128 rows (dq), or keys (dk, dv) and the parts of their rows
+  float* stat;         // [-lse, delta][batch][heads][q_len], the first in the domain of the scores
+  float* part;         // parts > 1: [head][tile][part][dk, dv][128][d]
 };
+
+// Nothing is moved across, where registers are short.
+template <bool TIGHT> __device__ inline void phase() {
+  if (TIGHT) __builtin_amdgcn_sched_barrier(0);
+}
 
 // A score and what its gradient is multiplied by.
 template <typename T, int MOD> struct Scorer {
@@ -104,22 +109,31 @@ template <typename T, int D, int MOD>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(Masked p, Plan plan) {
   using G = Geo<T, D>;
   constexpr int TILEB = G::TILEB, NDT = G::NDT;
+  constexpr bool TIGHT = sizeof(T) == 2 && D == 128;
   __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * TILEB];      // K0 | V0 | K1 | V1
+  constexpr bool MENDS = sizeof(T) == 2;
   __shared__ int span_s[4][4];
   __shared__ unsigned bad[2];
+  __shared__ unsigned heavy[MENDS ? (1 << kHeavyBits) / 32 : 1];       // tiles of this walk (or runs of them) with large weights
 
-  const int item = item_of_xcd(plan.per_xcd);
-  if ((int)(blockIdx.x / 8) >= plan.per_xcd || item >= plan.total) return;
-  const int bh = item / plan.n_tiles, b = bh / p.heads, head = bh % p.heads;
-  const int qt = p.causal ? plan.n_tiles - 1 - item % plan.n_tiles : item % plan.n_tiles;
+  __shared__ int32_t docs_s[kDocsInLds + 1];
+  __shared__ int size_s[kRankedTiles + 1];
+
+  const Share share = share_of(plan.deal);
+  if (share.head < 0) return;
+  const int bh = share.head, b = bh / p.heads, head = bh % p.heads;
+  const int32_t* offs = borders_of(p, b, docs_s);
+  const int qt = tile_of_rank<false>(p, offs, b, share.rank, plan.deal.n_tiles, size_s);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lam = lane & 31, h = lane >> 5;
   const int row = qt * kOwn + 32 * wave + lam;
   Interval iv{0, 0};
-  if (row < p.q_len) iv = keys_of_row(p, b, row);
+  if (row < p.q_len) iv = keys_of_row(p, offs, b, row);
   const bool sees = iv.lo < iv.hi;
   const Span ws = span_of_wave(iv);
   if (tid < 2) bad[tid] = 0u;
+  if (MENDS)
+    for (int i = tid; i < (1 << kHeavyBits) / 32; i += 256) heavy[i] = 0u;
   const Span gs = span_of_group(ws, span_s, wave, lane);
 
   const unsigned char* kg = p.k + b * p.sk.batch + (head / p.group) * p.sk.head;
@@ -158,7 +172,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
     }
     delta += __shfl_xor(delta, 32);
     if (sees) minus_lse = -in_domain<T>(p.lse[(size_t)bh * p.q_len + row]);
-    if (row < p.q_len && h == 0) plan.delta[(size_t)bh * p.q_len + row] = delta;
   }
   const Scorer<T, MOD> sc(p, head);
   const int pos = row + p.kv_len - p.q_len;
@@ -166,6 +179,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
   f32x16 acc[NDT];
 #pragma unroll
   for (int dt = 0; dt < NDT; ++dt) acc[dt] = (f32x16){0};
+  // bf16: delta from a rounded out is off by e = -sum_j dz_ij (the sum is 0 otherwise), and dq by -e sum_j p_ij k_j, which is
+  // as much as the other roundings together where few keys have most of a row's weight.  e is known when the walk is done;
+  // the tiles with weights of kHeavy and more are then walked once more for that sum (below kHeavy the rest does not
+  // matter: the sum falls with the number of keys that share the weight, and so does e).
+  float off = 0.f;
+  const int heavy_shift = MENDS ? max(0, 32 - __builtin_clz(max(t_end - t_begin, 1) - 1 | 1) - kHeavyBits) : 0;
 
   for (int t = t_begin; t < t_end; ++t) {
     const int par = (t - t_begin) & 1;
@@ -179,10 +198,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
     }
     if (!touches(ws, t * kRows, kRows)) continue;
     const bool part = !covers(ws, t * kRows, kRows);
+    float top = 0.f;
     auto half = [&](auto row0_tag) {
       constexpr int ROW0 = decltype(row0_tag)::value;
+      int lo = iv.lo;                            // addresses and key numbers are made anew, see masked_dkv_kernel
+      if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols[0]), "+v"(rd.cols[1]), "+v"(lo));
       const f32x16 s = rows_times<T, D, ROW0>(rd, k_off, q);
       const f32x16 dp = rows_times<T, D, ROW0>(rd, v_off, g);
+      phase<TIGHT>();
       Weights<T> w;
       const unsigned n = (unsigned)(iv.hi - iv.lo);
       const int key0 = t * kRows + ROW0 + 4 * h;
@@ -193,47 +216,118 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
         for (int u = 0; u < 2; ++u) {
           const int key = key0 + ((r + u) / 4) * 8 + (r + u) % 4;
           float gain;
-          const float wt = sc.weight(s[r + u], minus_lse, fabsf((float)(pos - key)), &gain);
+          float wt = sc.weight(s[r + u], minus_lse, fabsf((float)(pos - key)), &gain);
           x[u] = wt * (dp[r + u] - delta);
+          if (part && (unsigned)(key - lo) >= n) wt = x[u] = 0.f;
+          if (MENDS) {
+            off += x[u];
+            top = fmaxf(top, wt);
+          }
           if (MOD & CAP) x[u] *= gain;
-          if (part && (unsigned)(key - iv.lo) >= n) x[u] = 0.f;
         }
         w.set(r, x[0], x[1]);
       }
+      phase<TIGHT>();
       cols_times<T, D, ROW0>(rd, k_off, w, acc);
     };
     half(std::integral_constant<int, 0>{});
+    phase<TIGHT>();
     half(std::integral_constant<int, 32>{});
+    if (MENDS && __any(top >= kHeavy) && lane == 0) {
+      const int at = (t - t_begin) >> heavy_shift;
+      atomicOr(&heavy[at >> 5], 1u << (at & 31));
+    }
+  }
+  if constexpr (MENDS) {
+    off += __shfl_xor(off, 32);
+    delta += off;
+    __syncthreads();
+    for (int t = t_begin; t < t_end; ++t) {
+      const int at = (t - t_begin) >> heavy_shift;
+      const unsigned word = __builtin_amdgcn_readfirstlane(heavy[at >> 5]);
+      if (!(word >> (at & 31) & 1u)) {           // uniform over the workgroup
+        if (word == 0u && heavy_shift == 0) t += 31 - (at & 31);
+        continue;
+      }
+      __syncthreads();                           // the tile before has been read
+      lk.load(wave, lane, kg + (long long)t * kRows * p.sk.token, p.kv_len - t * kRows, lds);
+      wait_loads();
+      __syncthreads();
+      if (!covers(gs, t * kRows, kRows)) {
+        clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0], (LDS_PTR(unsigned))&bad[0], tid);
+        __syncthreads();
+      }
+      if (!touches(ws, t * kRows, kRows)) continue;
+      const bool part = !covers(ws, t * kRows, kRows);
+      auto half = [&](auto row0_tag) {
+        constexpr int ROW0 = decltype(row0_tag)::value;
+        int lo = iv.lo;
+        if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols[0]), "+v"(rd.cols[1]), "+v"(lo));
+        const f32x16 s = rows_times<T, D, ROW0>(rd, 0, q);
+        phase<TIGHT>();
+        Weights<T> w;
+        const unsigned n = (unsigned)(iv.hi - iv.lo);
+        const int key0 = t * kRows + ROW0 + 4 * h;
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+          float x[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int key = key0 + ((r + u) / 4) * 8 + (r + u) % 4;
+            float gain;
+            x[u] = -off * sc.weight(s[r + u], minus_lse, fabsf((float)(pos - key)), &gain);
+            if (MOD & CAP) x[u] *= gain;
+            if (part && (unsigned)(key - lo) >= n) x[u] = 0.f;
+          }
+          w.set(r, x[0], x[1]);
+        }
+        phase<TIGHT>();
+        cols_times<T, D, ROW0>(rd, 0, w, acc);
+      };
+      half(std::integral_constant<int, 0>{});
+      phase<TIGHT>();
+      half(std::integral_constant<int, 32>{});
+    }
+  }
+  if (row < p.q_len && h == 0) {
+    float* st = plan.stat + (size_t)bh * p.q_len + row;
+    st[0] = minus_lse;
+    st[(size_t)p.batch * p.heads * p.q_len] = sees ? delta : 0.f;
   }
   if (row < p.q_len)
     store_row<T, D>(p.dq + b * p.sdq.batch + head * p.sdq.head + (long long)row * p.sdq.token, acc, p.scale, sees, h);
 }
 
 template <typename T, int D, int MOD>
-__global__ __launch_bounds__(256, 1) void masked_dkv_kernel(Masked p, Plan plan) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel(Masked p, Plan plan) {
   using G = Geo<T, D>;
   constexpr int TILEB = G::TILEB, NDT = G::NDT;
+  constexpr bool TIGHT = sizeof(T) == 2 && D == 128;
   __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * TILEB];      // Q0 | dO0 | Q1 | dO1
   __shared__ __attribute__((aligned(16))) float stat[2][2][kRows];               // [parity][-lse, delta][row]
   __shared__ int span_s[4][4];
   __shared__ unsigned bad[2];
 
-  const int item = item_of_xcd(plan.per_xcd);
-  if ((int)(blockIdx.x / 8) >= plan.per_xcd || item >= plan.total) return;
-  const int part_no = item % plan.n_parts, unit = item / plan.n_parts;
-  const int bk = unit / plan.n_tiles, b = bk / p.kv_heads, kv_head = bk % p.kv_heads;
-  const int kt = unit % plan.n_tiles;
+  __shared__ int32_t docs_s[kDocsInLds + 1];
+  __shared__ int size_s[kRankedTiles + 1];
+
+  const Share share = share_of(plan.deal);
+  if (share.head < 0) return;
+  const int bk = share.head, b = bk / p.kv_heads, kv_head = bk % p.kv_heads;
+  const int32_t* offs = borders_of(p, b, docs_s);
+  const int kt = tile_of_rank<true>(p, offs, b, share.rank, plan.deal.n_tiles, size_s);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lam = lane & 31, h = lane >> 5;
   const int key = kt * kOwn + 32 * wave + lam;
   Interval iv{0, 0};
-  if (key < p.kv_len) iv = rows_of_key(p, b, key);
+  if (key < p.kv_len) iv = rows_of_key(p, offs, b, key);
   const bool seen = iv.lo < iv.hi;
   const Span ws = span_of_wave(iv);
   if (tid < 2) bad[tid] = 0u;
   const Span gs = span_of_group(ws, span_s, wave, lane);
 
   const unsigned lds = (unsigned)(unsigned long long)(LDS_PTR(unsigned char)) & stage[0];
+  const unsigned lds_stat = (unsigned)(unsigned long long)(LDS_PTR(float)) & stat[0][0][0];
   Loader<T, D> lq, lg;
   lq.init(wave, lane, (unsigned)p.sq.token);
   lg.init(wave, lane, (unsigned)p.sdo.token);
@@ -247,18 +341,22 @@ __global__ __launch_bounds__(256, 1) void masked_dkv_kernel(Masked p, Plan plan)
     n = (gs.hi + kRows - 1) / kRows - t_begin;
   }
   const long long steps = (long long)n * p.group;
-  const int i_begin = (int)(steps * part_no / plan.n_parts), i_end = (int)(steps * (part_no + 1) / plan.n_parts);
-  auto load = [&](int i, int par) {
-    const int head = kv_head * p.group + i / n, t = t_begin + i % n;
+  const int i_begin = (int)(steps * share.part / plan.deal.n_parts), i_end = (int)(steps * (share.part + 1) / plan.deal.n_parts);
+  int head = kv_head * p.group, t = t_begin;     // of the tile that is loaded next
+  if (n > 0) {
+    head += i_begin / n;
+    t += i_begin % n;
+  }
+  const size_t all_rows = (size_t)p.batch * p.heads * p.q_len;
+  auto load = [&](int par) {
     const int avail = p.q_len - t * kRows;
+    if (wave < 2) {
+      const float* st = plan.stat + wave * all_rows + ((size_t)b * p.heads + head) * p.q_len + t * kRows;
+      dma_words(lds_stat + (par * 2 + wave) * (kRows * 4), (unsigned)(min(lane, avail - 1) * 4), st);
+    }
     lq.load(wave, lane, p.q + b * p.sq.batch + head * p.sq.head + (long long)t * kRows * p.sq.token, avail, lds + 2 * par * TILEB);
     lg.load(wave, lane, p.dout + b * p.sdo.batch + head * p.sdo.head + (long long)t * kRows * p.sdo.token, avail,
             lds + (2 * par + 1) * TILEB);
-  };
-  auto fetch_stat = [&](int i) -> float {        // threads 0..63: -lse, 64..127: delta
-    const int head = kv_head * p.group + i / n, t = t_begin + i % n;
-    const size_t at = ((size_t)b * p.heads + head) * p.q_len + min(t * kRows + (tid & 63), p.q_len - 1);
-    return wave == 0 ? -in_domain<T>(p.lse[at]) : plan.delta[at];
   };
 
   u32x4 k[G::STEPS], v[G::STEPS];
@@ -278,36 +376,41 @@ __global__ __launch_bounds__(256, 1) void masked_dkv_kernel(Masked p, Plan plan)
 #pragma unroll
   for (int dt = 0; dt < NDT; ++dt) dk[dt] = dv[dt] = (f32x16){0};
 
-  if (i_begin < i_end) {
-    if (wave < 2) stat[0][wave][lane] = fetch_stat(i_begin);
-    load(i_begin, 0);
-  }
+  if (i_begin < i_end) load(0);
   const int shift = p.kv_len - p.q_len;
   for (int i = i_begin; i < i_end; ++i) {
     const int par = (i - i_begin) & 1;
     const unsigned q_off = 2 * par * TILEB, g_off = q_off + TILEB;
-    const int t = t_begin + i % n;
+    const int x0 = t * kRows, head_now = head;
     wait_loads();
     __syncthreads();
     if (i + 1 < i_end) {
-      load(i + 1, par ^ 1);
-      if (wave < 2) stat[par ^ 1][wave][lane] = fetch_stat(i + 1);
+      if (++t == t_begin + n) {
+        t = t_begin;
+        ++head;
+      }
+      load(par ^ 1);
     }
-    if (!covers(gs, t * kRows, kRows)) {         // both second products contract over rows that do not all see every key
+    if (!covers(gs, x0, kRows)) {         // both second products contract over rows that do not all see every key
       clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0] + q_off, (LDS_PTR(unsigned))&bad[0], tid);
       clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0] + g_off, (LDS_PTR(unsigned))&bad[0], tid);
       __syncthreads();
     }
-    if (!touches(ws, t * kRows, kRows)) continue;
-    const bool part = !covers(ws, t * kRows, kRows);
-    const Scorer<T, MOD> sc(p, kv_head * p.group + i / n);
+    if (!touches(ws, x0, kRows)) continue;
+    const bool part = !covers(ws, x0, kRows);
+    const Scorer<T, MOD> sc(p, head_now);
     auto half = [&](auto row0_tag) {
       constexpr int ROW0 = decltype(row0_tag)::value;
+      // 192 of 256 registers hold k, v, dk and dv: addresses and row numbers are made anew where they are wanted, and the
+      // products are kept apart from what follows, or the scheduler spills to feed them early
+      int lo = iv.lo;
+      if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols[0]), "+v"(rd.cols[1]), "+v"(lo));
       const f32x16 s = rows_times<T, D, ROW0>(rd, q_off, k);
       const f32x16 dp = rows_times<T, D, ROW0>(rd, g_off, v);
+      phase<TIGHT>();
       Weights<T> wp, wd;
       const unsigned count = (unsigned)(iv.hi - iv.lo);
-      const int row0 = t * kRows + ROW0 + 4 * h;
+      const int row0 = x0 + ROW0 + 4 * h;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const f32x4 ml = *reinterpret_cast<LDS_PTR(const f32x4)>((LDS_PTR(const float))&stat[par][0][ROW0 + 8 * e + 4 * h]);
@@ -322,7 +425,7 @@ __global__ __launch_bounds__(256, 1) void masked_dkv_kernel(Masked p, Plan plan)
           if (MOD & CAP) y[u] *= gain;
           if (part) {
             x[u] = fmaf(0.f, de[u], x[u]);       // a row of dout that was cleaned of inf or NaN has a delta of NaN
-            if ((unsigned)(row - iv.lo) >= count) x[u] = y[u] = 0.f;
+            if ((unsigned)(row - lo) >= count) x[u] = y[u] = 0.f;
           }
         }
         wp.set(4 * e, x[0], x[1]);
@@ -330,15 +433,18 @@ __global__ __launch_bounds__(256, 1) void masked_dkv_kernel(Masked p, Plan plan)
         wd.set(4 * e, y[0], y[1]);
         wd.set(4 * e + 2, y[2], y[3]);
       }
+      phase<TIGHT>();
       cols_times<T, D, ROW0>(rd, g_off, wp, dv);
       cols_times<T, D, ROW0>(rd, q_off, wd, dk);
     };
     half(std::integral_constant<int, 0>{});
+    phase<TIGHT>();
     half(std::integral_constant<int, 32>{});
   }
 
-  if (plan.n_parts > 1) {
-    unsigned char* dst = reinterpret_cast<unsigned char*>(plan.part + ((size_t)item * 2 * kOwn + 32 * wave + lam) * D);
+  if (plan.deal.n_parts > 1) {
+    const size_t item = ((size_t)bk * plan.deal.n_tiles + kt) * plan.deal.n_parts + share.part;
+    unsigned char* dst = reinterpret_cast<unsigned char*>(plan.part + (item * 2 * kOwn + 32 * wave + lam) * D);
     store_row<float, D>(dst, dk, p.scale, seen, h);
     store_row<float, D>(dst + (size_t)kOwn * D * sizeof(float), dv, 1.f, seen, h);
     return;
@@ -353,12 +459,12 @@ __global__ __launch_bounds__(256, 1) void masked_dkv_kernel(Masked p, Plan plan)
 template <typename T, int D> __global__ __launch_bounds__(256) void masked_dkv_join_kernel(Masked p, Plan plan) {
   constexpr int PER_ROW = D / 4, ROWS = 256 / PER_ROW;
   const int unit = blockIdx.y, tid = threadIdx.x, which = blockIdx.z;
-  const int bk = unit / plan.n_tiles, b = bk / p.kv_heads, kv_head = bk % p.kv_heads;
-  const int r = blockIdx.x * ROWS + tid / PER_ROW, ch = 4 * (tid % PER_ROW), key = unit % plan.n_tiles * kOwn + r;
+  const int bk = unit / plan.deal.n_tiles, b = bk / p.kv_heads, kv_head = bk % p.kv_heads;
+  const int r = blockIdx.x * ROWS + tid / PER_ROW, ch = 4 * (tid % PER_ROW), key = unit % plan.deal.n_tiles * kOwn + r;
   if (key >= p.kv_len) return;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < plan.n_parts; ++i)
-    sum += *reinterpret_cast<const f32x4*>(plan.part + ((((size_t)unit * plan.n_parts + i) * 2 + which) * kOwn + r) * D + ch);
+  for (int i = 0; i < plan.deal.n_parts; ++i)
+    sum += *reinterpret_cast<const f32x4*>(plan.part + ((((size_t)unit * plan.deal.n_parts + i) * 2 + which) * kOwn + r) * D + ch);
   const Strides& sd = which ? p.sdv : p.sdk;
   unsigned char* dst = (which ? p.dv : p.dk) + b * sd.batch + kv_head * sd.head + (long long)key * sd.token;
   if constexpr (sizeof(T) == 2)
@@ -367,37 +473,36 @@ template <typename T, int D> __global__ __launch_bounds__(256) void masked_dkv_j
     *reinterpret_cast<f32x4*>(dst + 4 * ch) = sum;
 }
 
+int tiles_of(int n) { return (n + kOwn - 1) / kOwn; }
 Plan plan_q(const Masked& m) {
   Plan pl{};
-  pl.n_tiles = (m.q_len + kOwn - 1) / kOwn;
-  pl.n_parts = 1;
-  pl.total = m.batch * m.heads * pl.n_tiles;
-  pl.per_xcd = (pl.total + 7) / 8;
+  pl.deal = deal_of(m.batch * m.heads, tiles_of(m.q_len), 1, m.dtype == PISA_BF16 ? 64 : 32);
   return pl;
 }
 Plan plan_kv(const Masked& m) {
   Plan pl{};
-  pl.n_tiles = (m.kv_len + kOwn - 1) / kOwn;
-  const long long units = (long long)m.batch * m.kv_heads * pl.n_tiles;
+  const long long units = (long long)m.batch * m.kv_heads * tiles_of(m.kv_len);
   if (units == 0) return pl;
-  // Rows are shared out where the key tiles alone leave compute units idle.
+  // A key tile's rows are shared out where the tiles alone do not fill two rounds of the 512 places on the card (backward pass,
+  // us, whole / shared out: 2 x 4 key heads of 2 777, 64 channels, 583 / 259; 13 heads of 6 000, causal, 988 / 845).  Causal
+  // tiles differ in size and leave places idle for longer: up to 800 (12 of 8 192 1 112 / 1 018), the others up to 640 (24 of
+  // 4 000 in documents, 768 tiles, 323 / 352).
   const long long steps = (long long)m.group * ((m.q_len + kRows - 1) / kRows);
-  long long parts = units >= 256 ? 1 : 256 / units;
+  long long parts = units >= (m.causal ? 800 : 640) ? 1 : (1024 + units - 1) / units;
   parts = parts < steps / 4 ? parts : steps / 4;
-  pl.n_parts = parts < 1 ? 1 : (int)parts;
-  pl.total = (int)(units * pl.n_parts);
-  pl.per_xcd = (pl.total + 7) / 8;
+  pl.deal = deal_of(m.batch * m.kv_heads, tiles_of(m.kv_len), parts < 1 ? 1 : (int)parts, m.dtype == PISA_BF16 ? 64 : 32);
   return pl;
 }
+size_t items_of(const Plan& pl, const Masked& m) { return (size_t)m.batch * m.kv_heads * pl.deal.n_tiles * pl.deal.n_parts; }
 
 template <typename T, int D, int MOD> hipError_t launch_mod(const Masked& m, const Plan& pq, const Plan& pk, hipStream_t stream) {
-  hipLaunchKernelGGL((masked_dq_kernel<T, D, MOD>), dim3(8 * pq.per_xcd), dim3(256), 0, stream, m, pq);
+  hipLaunchKernelGGL((masked_dq_kernel<T, D, MOD>), dim3(8 * pq.deal.per_xcd), dim3(256), 0, stream, m, pq);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || pk.total == 0) return e;
-  hipLaunchKernelGGL((masked_dkv_kernel<T, D, MOD>), dim3(8 * pk.per_xcd), dim3(256), 0, stream, m, pk);
+  if (e != hipSuccess || m.kv_len == 0) return e;
+  hipLaunchKernelGGL((masked_dkv_kernel<T, D, MOD>), dim3(8 * pk.deal.per_xcd), dim3(256), 0, stream, m, pk);
   e = hipGetLastError();
-  if (e != hipSuccess || pk.n_parts == 1) return e;
-  hipLaunchKernelGGL((masked_dkv_join_kernel<T, D>), dim3(kOwn / (256 / (D / 4)), pk.total / pk.n_parts, 2), dim3(256), 0, stream, m, pk);
+  if (e != hipSuccess || pk.deal.n_parts == 1) return e;
+  hipLaunchKernelGGL((masked_dkv_join_kernel<T, D>), dim3(kOwn / (256 / (D / 4)), m.batch * m.kv_heads * pk.deal.n_tiles, 2), dim3(256), 0, stream, m, pk);
   return hipGetLastError();
 }
 template <typename T, int D> hipError_t launch_td(const Masked& m, const Plan& pq, const Plan& pk, hipStream_t stream) {
@@ -409,19 +514,19 @@ template <typename T, int D> hipError_t launch_td(const Masked& m, const Plan& p
   }
 }
 
-size_t delta_bytes(const Masked& m) { return ((size_t)m.batch * m.heads * m.q_len * sizeof(float) + 255) & ~(size_t)255; }
+size_t stat_bytes(const Masked& m) { return (2 * (size_t)m.batch * m.heads * m.q_len * sizeof(float) + 255) & ~(size_t)255; }
 
 }  // namespace
 
 size_t masked_backward_workspace_bytes(const Masked& m) {
   const Plan pk = plan_kv(m);
-  return delta_bytes(m) + (pk.n_parts > 1 ? (size_t)pk.total * 2 * kOwn * m.d * sizeof(float) : 0);
+  return stat_bytes(m) + (pk.deal.n_parts > 1 ? items_of(pk, m) * 2 * kOwn * m.d * sizeof(float) : 0);
 }
 
 hipError_t launch_masked_backward(const Masked& m, hipStream_t stream) {
   Plan pq = plan_q(m), pk = plan_kv(m);
-  pq.delta = pk.delta = static_cast<float*>(m.workspace);
-  pk.part = reinterpret_cast<float*>(static_cast<unsigned char*>(m.workspace) + delta_bytes(m));
+  pq.stat = pk.stat = static_cast<float*>(m.workspace);
+  pk.part = reinterpret_cast<float*>(static_cast<unsigned char*>(m.workspace) + stat_bytes(m));
   if (m.dtype == PISA_BF16) return m.d == 64 ? launch_td<__bf16, 64>(m, pq, pk, stream) : launch_td<__bf16, 128>(m, pq, pk, stream);
   return m.d == 64 ? launch_td<float, 64>(m, pq, pk, stream) : launch_td<float, 128>(m, pq, pk, stream);
 }

@@ -19,11 +19,9 @@ constexpr int kQRows = 128;
 constexpr int CAP = 1, BIAS = 2;         // bits of MOD: scores capped, biased by distance
 
 struct Plan {
-  int n_qt;            // tiles of 128 rows to a head
-  int n_parts;         // workgroups that share a tile's keys
-  int total, per_xcd;  // items: (batch, head, tile, part)
-  float* part_o;       // n_parts > 1: [item][128][d] sums of weighted values, before division
-  float* part_ml;      // [item][2][128] maximum and sum of weights
+  Deal deal;           // of tiles of 128 rows; parts: workgroups that share a tile's keys
+  float* part_o;       // parts > 1: [head][tile][part][128][d] sums of weighted values, before division
+  float* part_ml;      // [head][tile][part][2][128] maximum and sum of weights
 };
 
 template <typename T, int D> struct Row {        // what a lane holds of its query row
@@ -69,17 +67,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
   __shared__ int span_s[4][4];
   __shared__ unsigned bad[2];
 
-  const int item = item_of_xcd(plan.per_xcd);
-  if ((int)(blockIdx.x / 8) >= plan.per_xcd || item >= plan.total) return;
-  const int part = item % plan.n_parts, unit = item / plan.n_parts;
-  const int bh = unit / plan.n_qt, b = bh / p.heads, head = bh % p.heads;
-  const int qt = p.causal ? plan.n_qt - 1 - unit % plan.n_qt : unit % plan.n_qt;     // the tiles with most keys first
+  __shared__ int32_t docs_s[kDocsInLds + 1];
+  __shared__ int size_s[kRankedTiles + 1];
+
+  const Share share = share_of(plan.deal);
+  if (share.head < 0) return;
+  const int bh = share.head, b = bh / p.heads, head = bh % p.heads;
+  const int32_t* offs = borders_of(p, b, docs_s);
+  const int qt = tile_of_rank<false>(p, offs, b, share.rank, plan.deal.n_tiles, size_s);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lam = lane & 31, h = lane >> 5;
 
   const int row = qt * kQRows + 32 * wave + lam;
   Interval iv{0, 0};
-  if (row < p.q_len) iv = keys_of_row(p, b, row);
+  if (row < p.q_len) iv = keys_of_row(p, offs, b, row);
   const bool sees = iv.lo < iv.hi;
   const Span ws = span_of_wave(iv);
   if (lane == 0) {
@@ -132,10 +133,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
     t_begin = gs.lo / kRows;
     t_end = (gs.hi + kRows - 1) / kRows;
   }
-  if (plan.n_parts > 1) {
+  if (plan.deal.n_parts > 1) {
     const int n = t_end - t_begin, first = t_begin;
-    t_begin = first + (int)((long long)n * part / plan.n_parts);
-    t_end = first + (int)((long long)n * (part + 1) / plan.n_parts);
+    t_begin = first + (int)((long long)n * share.part / plan.deal.n_parts);
+    t_end = first + (int)((long long)n * (share.part + 1) / plan.deal.n_parts);
   }
 
   auto load_k = [&](int t, int stage_at) {
@@ -249,7 +250,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
   }
 
   st.l += __shfl_xor(st.l, 32);
-  if (plan.n_parts > 1) {
+  if (plan.deal.n_parts > 1) {
+    const size_t item = ((size_t)bh * plan.deal.n_tiles + qt) * plan.deal.n_parts + share.part;
     float* po = plan.part_o + ((size_t)item * kQRows + 32 * wave + lam) * D;
 #pragma unroll
     for (int dt = 0; dt < NDT; ++dt)
@@ -287,16 +289,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
 // Joins the parts of 128 rows: a thread has four channels of a row.  Workgroup: (batch, head, tile) x slices of its rows.
 template <typename T, int D> __global__ __launch_bounds__(256) void masked_join_kernel(Masked p, Plan plan) {
   constexpr int PER_ROW = D / 4, ROWS = 256 / PER_ROW;
-  const int unit = blockIdx.y, tid = threadIdx.x;
-  const int bh = unit / plan.n_qt, b = bh / p.heads, head = bh % p.heads;
-  const int qt = p.causal ? plan.n_qt - 1 - unit % plan.n_qt : unit % plan.n_qt;
+  const int unit = blockIdx.y, tid = threadIdx.x, n_parts = plan.deal.n_parts;
+  const int bh = unit / plan.deal.n_tiles, b = bh / p.heads, head = bh % p.heads, qt = unit % plan.deal.n_tiles;
   const int r = blockIdx.x * ROWS + tid / PER_ROW, ch = 4 * (tid % PER_ROW), row = qt * kQRows + r;
   if (row >= p.q_len) return;
-  const size_t item = (size_t)unit * plan.n_parts;
+  const size_t item = (size_t)unit * n_parts;
   float m = -INFINITY, l = 0.f;
-  for (int i = 0; i < plan.n_parts; ++i) m = fmaxf(m, plan.part_ml[((item + i) * 2) * kQRows + r]);
+  for (int i = 0; i < n_parts; ++i) m = fmaxf(m, plan.part_ml[((item + i) * 2) * kQRows + r]);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < plan.n_parts; ++i) {
+  for (int i = 0; i < n_parts; ++i) {
     const float li = plan.part_ml[((item + i) * 2 + 1) * kQRows + r];
     if (li == 0.f) continue;                     // no key of the row in this part
     const float f = exp_of<T>(plan.part_ml[((item + i) * 2) * kQRows + r] - m);
@@ -315,23 +316,24 @@ template <typename T, int D> __global__ __launch_bounds__(256) void masked_join_
   if (p.lse && ch == 0) p.lse[(size_t)bh * p.q_len + row] = sees ? log_sum<T>(m, l) : -INFINITY;
 }
 
-Plan plan_of(const Masked& m) {
-  Plan pl{};
-  pl.n_qt = (m.q_len + kQRows - 1) / kQRows;
-  const long long units = (long long)m.batch * m.heads * pl.n_qt;
+int parts_of(const Masked& m) {
+  const long long units = (long long)m.batch * m.heads * ((m.q_len + kQRows - 1) / kQRows);
   // Keys are shared out where the tiles alone leave compute units idle and there are keys enough to share.
   const long long slots = m.dtype == PISA_BF16 ? 512 : 256;
   const int tiles = (m.kv_len + kRows - 1) / kRows;
   long long parts = units >= slots ? 1 : slots / units;
   parts = parts < tiles / 4 ? parts : tiles / 4;
-  pl.n_parts = parts < 1 ? 1 : (int)parts;
-  pl.total = (int)(units * pl.n_parts);
-  pl.per_xcd = (pl.total + 7) / 8;
+  return parts < 1 ? 1 : (int)parts;
+}
+size_t items_of(const Plan& pl, const Masked& m) { return (size_t)m.batch * m.heads * pl.deal.n_tiles * pl.deal.n_parts; }
+Plan plan_of(const Masked& m) {
+  Plan pl{};
+  pl.deal = deal_of(m.batch * m.heads, (m.q_len + kQRows - 1) / kQRows, parts_of(m), m.dtype == PISA_BF16 ? 64 : 32);
   return pl;
 }
 
 template <typename T, int D> hipError_t launch_td(const Masked& m, const Plan& pl, hipStream_t stream) {
-  const dim3 grid(8 * pl.per_xcd), block(256);
+  const dim3 grid(8 * pl.deal.per_xcd), block(256);
   switch ((m.cap > 0.f ? CAP : 0) | (m.slopes ? BIAS : 0)) {
     case 0: hipLaunchKernelGGL((masked_fwd_kernel<T, D, 0>), grid, block, 0, stream, m, pl); break;
     case CAP: hipLaunchKernelGGL((masked_fwd_kernel<T, D, CAP>), grid, block, 0, stream, m, pl); break;
@@ -339,8 +341,8 @@ template <typename T, int D> hipError_t launch_td(const Masked& m, const Plan& p
     default: hipLaunchKernelGGL((masked_fwd_kernel<T, D, CAP | BIAS>), grid, block, 0, stream, m, pl); break;
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || pl.n_parts == 1) return e;
-  hipLaunchKernelGGL((masked_join_kernel<T, D>), dim3(kQRows / (256 / (D / 4)), pl.total / pl.n_parts), block, 0, stream, m, pl);
+  if (e != hipSuccess || pl.deal.n_parts == 1) return e;
+  hipLaunchKernelGGL((masked_join_kernel<T, D>), dim3(kQRows / (256 / (D / 4)), m.batch * m.heads * pl.deal.n_tiles), block, 0, stream, m, pl);
   return hipGetLastError();
 }
 
@@ -348,14 +350,14 @@ template <typename T, int D> hipError_t launch_td(const Masked& m, const Plan& p
 
 size_t masked_workspace_bytes(const Masked& m) {
   const Plan pl = plan_of(m);
-  return pl.n_parts == 1 ? 0 : (size_t)pl.total * kQRows * (m.d + 2) * sizeof(float);
+  return pl.deal.n_parts == 1 ? 0 : items_of(pl, m) * kQRows * (m.d + 2) * sizeof(float);
 }
 
 hipError_t launch_masked_attention(const Masked& m, hipStream_t stream) {
   Plan pl = plan_of(m);
-  if (pl.n_parts > 1) {
+  if (pl.deal.n_parts > 1) {
     pl.part_o = static_cast<float*>(m.workspace);
-    pl.part_ml = pl.part_o + (size_t)pl.total * kQRows * m.d;
+    pl.part_ml = pl.part_o + items_of(pl, m) * kQRows * m.d;
   }
   if (m.dtype == PISA_BF16) return m.d == 64 ? launch_td<__bf16, 64>(m, pl, stream) : launch_td<__bf16, 128>(m, pl, stream);
   return m.d == 64 ? launch_td<float, 64>(m, pl, stream) : launch_td<float, 128>(m, pl, stream);

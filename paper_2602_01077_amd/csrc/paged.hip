@@ -37,7 +37,9 @@ struct PPlan {
   int blocks;          // of 16 query heads to a key head
   float* part_o;       // [workgroup][2][16][d] weighted values: of its first unit, of its last
   float* part_ml;      // [workgroup][2][2][16] maximum and sum
+  int32_t* owners;     // [seq][unit][2] first and last workgroup; the first's slot is its second if the last has bit 30 set
 };
+constexpr int kSecondSlot = 1 << 30;
 
 // What rows of masked keys are read from: weight 0 times a row of a foreign or unwritten page could be NaN.
 __device__ const u32x4 zero_row[32] = {};
@@ -45,16 +47,6 @@ __device__ const u32x4 zero_row[32] = {};
 __device__ inline int length_of(const Paged& p, int s) {
   const long long most = (long long)p.max_pages * p.page_size;
   return (int)min((long long)max(p.lengths[s], 0), most);
-}
-
-// Sum over the workgroup; all threads get it.
-__device__ inline long long sum_of(long long x, long long* scratch /* 4 */) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = x;
-  __syncthreads();
-  return scratch[0] + scratch[1] + scratch[2] + scratch[3];
 }
 
 // First tile of workgroup w's range: total * w / n (n workgroups take part).
@@ -99,35 +91,46 @@ __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(
   const int j = lane & 15, g = lane >> 4;
 
   // ---- this workgroup's range of tiles, and the sequence it starts in ----
-  long long mine = 0;
-  for (int s = tid; s < p.seqs; s += 256) mine += (length_of(p, s) + P::TILE - 1) / P::TILE;
-  const long long total = sum_of(mine, scratch) * plan.units;
+  // tiles up to and with sequence s0 + tid, from s0; *all: of the 256 sequences
+  auto scan = [&](int s0, long long* all) {
+    const int s = s0 + tid;
+    long long incl = s < p.seqs ? (length_of(p, s) + P::TILE - 1) / P::TILE : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const long long up = __shfl_up(incl, o);
+      if (lane >= o) incl += up;
+    }
+    __syncthreads();
+    if (lane == 63) scratch[wave] = incl;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) incl += scratch[w];
+    *all = scratch[0] + scratch[1] + scratch[2] + scratch[3];
+    return incl;
+  };
+  long long here = 0, incl = scan(0, &here), total = here;
+  for (int s0 = 256; s0 < p.seqs; s0 += 256) {
+    long long more;
+    scan(s0, &more);
+    total += more;
+  }
+  total *= plan.units;
   const int n_groups = (int)min((long long)P::GROUPS, total);
   if ((int)blockIdx.x >= n_groups) return;
   const long long x_begin = first_tile(total, n_groups, blockIdx.x), x_end = first_tile(total, n_groups, blockIdx.x + 1);
   {
-    long long base = 0;                          // tiles of the sequences before
-    for (int s0 = 0; s0 < p.seqs; s0 += 256) {
+    long long base = 0;                          // tiles of the sequences before s0
+    for (int s0 = 0;;) {
       const int s = s0 + tid;
       const long long t = s < p.seqs ? (length_of(p, s) + P::TILE - 1) / P::TILE : 0;
-      long long incl = t;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const long long up = __shfl_up(incl, o);
-        if (lane >= o) incl += up;
-      }
-      __syncthreads();
-      if (lane == 63) scratch[wave] = incl;
-      __syncthreads();
-      long long before = base;
-      for (int w = 0; w < wave; ++w) before += scratch[w];
-      const long long lo = (before + incl - t) * plan.units, hi = (before + incl) * plan.units;
+      const long long lo = (base + incl - t) * plan.units, hi = (base + incl) * plan.units;
       if (lo <= x_begin && x_begin < hi) {
         found_s[0] = s;
         found_s[1] = lo;
       }
-      base += scratch[0] + scratch[1] + scratch[2] + scratch[3];
-      if (base * plan.units > x_begin) break;    // uniform
+      base += here;
+      s0 += 256;
+      if (base * plan.units > x_begin || s0 >= p.seqs) break;      // uniform
+      incl = scan(s0, &here);
     }
     __syncthreads();
   }
@@ -336,6 +339,12 @@ __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(
             *reinterpret_cast<f32x4*>(p.out + (hd * D + ch0 + e) * 4) = acc;
         }
       }
+      if (t0 == 0 && tid == 0) {                 // who has this unit, for the launch that joins
+        const long long x1 = x + tiles - 1;
+        int32_t* own = plan.owners + ((size_t)seq * plan.units + unit) * 2;
+        own[0] = (int)blockIdx.x | (x == x_begin ? 0 : kSecondSlot);
+        own[1] = (int)(((x1 + 1) * n_groups - 1) / total);       // the last workgroup whose range starts at or before x1
+      }
       if (tid % 16 == 0) {
         if (!whole) {
           plan.part_ml[(slot * 2 + 0) * kCols + c] = top;
@@ -350,46 +359,58 @@ __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(
   }
 }
 
-// A workgroup to a (sequence, unit): nothing to do where one workgroup had all of it.
+// A workgroup to a (sequence, unit): nothing to do where one workgroup had all of it.  A thread has D / 16 channels of a row.
 template <typename T, int D> __global__ __launch_bounds__(256) void paged_join_kernel(Paged p, PPlan plan) {
-  using P = PGeo<T, D>;
-  __shared__ long long scratch[4];
   const int seq = blockIdx.x / plan.units, unit = blockIdx.x % plan.units, tid = threadIdx.x;
-  long long all = 0, below = 0;
-  for (int s = tid; s < p.seqs; s += 256) {
-    const long long t = (length_of(p, s) + P::TILE - 1) / P::TILE;
-    all += t;
-    if (s < seq) below += t;
-  }
-  const long long total = sum_of(all, scratch) * plan.units;
-  const long long before = sum_of(below, scratch) * plan.units;
-  const int n_groups = (int)min((long long)P::GROUPS, total);
-  const int tiles = (length_of(p, seq) + P::TILE - 1) / P::TILE;
-  const int kv_head = unit / plan.blocks, c = tid / 16, ch0 = (tid % 16) * (D / 16), r = unit % plan.blocks * kCols + c;
-  if (r >= p.group) return;
+  const int kv_head = unit / plan.blocks, c = tid / 16, j = tid % 16, ch0 = j * (D / 16), r = unit % plan.blocks * kCols + c;
+  const bool empty = length_of(p, seq) == 0;
+  const int2 own = *reinterpret_cast<const int2*>(plan.owners + (size_t)blockIdx.x * 2);
+  const int w0 = own.x & (kSecondSlot - 1), w1 = own.y;
+  if ((!empty && w0 == w1) || r >= p.group) return;
   const size_t hd = (size_t)seq * p.heads + kv_head * p.group + r;
 
   float top = -INFINITY, sum = 0.f;
   f32x4 acc[D / 64];
 #pragma unroll
   for (int e = 0; e < D / 64; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (tiles > 0) {
-    const long long x0 = before + (long long)unit * tiles, x1 = x0 + tiles;
-    // the workgroup that holds tile x is the last one whose range starts at or before it
-    const int w0 = (int)(((x0 + 1) * n_groups - 1) / total), w1 = (int)((x1 * n_groups - 1) / total);
-    if (w0 == w1) return;
-    for (int w = w0; w <= w1; ++w) {
-      const size_t slot = (size_t)w * 2 + (first_tile(total, n_groups, w) >= x0 ? 0 : 1);
-      top = fmaxf(top, plan.part_ml[(slot * 2) * kCols + c]);
-    }
-    for (int w = w0; w <= w1; ++w) {
-      const size_t slot = (size_t)w * 2 + (first_tile(total, n_groups, w) >= x0 ? 0 : 1);
-      const float li = plan.part_ml[(slot * 2 + 1) * kCols + c];
-      if (li == 0.f) continue;
-      const float f = exp_of<T>(plan.part_ml[(slot * 2) * kCols + c] - top);
-      sum += li * f;
+  if (!empty) {
+    // parts 16 at a time, one to each of a row's 16 threads for the maximum and the factor
+    auto slot_of = [&](int w) { return (size_t)w * 2 + (w == w0 && (own.x & kSecondSlot) ? 1 : 0); };
+    for (int w = w0; w <= w1; w += 16) {
+      float m = -INFINITY, l = 0.f;
+      if (w + j <= w1) {
+        m = plan.part_ml[slot_of(w + j) * 2 * kCols + c];
+        l = plan.part_ml[(slot_of(w + j) * 2 + 1) * kCols + c];
+      }
+      float t = m;
 #pragma unroll
-      for (int e = 0; e < D / 64; ++e) acc[e] += *reinterpret_cast<const f32x4*>(plan.part_o + (slot * kCols + c) * D + ch0 + 4 * e) * f;
+      for (int o = 1; o < 16; o <<= 1) t = fmaxf(t, __shfl_xor(t, o, 16));
+      const float m_new = fmaxf(top, t);
+      const float old = top == -INFINITY ? 0.f : exp_of<T>(top - m_new);
+      const float f = l == 0.f ? 0.f : exp_of<T>(m - m_new);
+      top = m_new;
+      float part = l * f;
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) part += __shfl_xor(part, o, 16);
+      sum = sum * old + part;
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) acc[e] *= old;
+      const int n = min(16, w1 - w + 1);
+      for (int i = 0; i < n; i += 4) {
+        f32x4 x[4][D / 64];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int e = 0; e < D / 64; ++e)
+            x[u][e] = *reinterpret_cast<const f32x4*>(plan.part_o + (slot_of(w + min(i + u, n - 1)) * kCols + c) * D + ch0 + 4 * e);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float g = __shfl(f, min(i + u, 15), 16);         // 0 past the last part
+          if (i + u < n && g != 0.f)
+#pragma unroll
+            for (int e = 0; e < D / 64; ++e) acc[e] += x[u][e] * g;
+        }
+      }
     }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -401,7 +422,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void paged_join_k
     else
       *reinterpret_cast<f32x4*>(p.out + (hd * D + ch0 + 4 * e) * 4) = y;
   }
-  if (p.lse && tid % 16 == 0) p.lse[hd] = sum == 0.f ? -INFINITY : log_sum<T>(top, sum);
+  if (p.lse && j == 0) p.lse[hd] = sum == 0.f ? -INFINITY : log_sum<T>(top, sum);
 }
 
 // A thread moves 16 bytes of one token's key or value row of one head.
@@ -459,12 +480,15 @@ template <typename T, int D> hipError_t launch_td(const Paged& p, const PPlan& p
 
 }  // namespace
 
-size_t paged_workspace_bytes(const Paged& p) { return (size_t)groups_of(p) * 2 * kCols * (p.d + 2) * sizeof(float); }
+size_t paged_workspace_bytes(const Paged& p) {
+  return (size_t)groups_of(p) * 2 * kCols * (p.d + 2) * sizeof(float) + (size_t)p.seqs * plan_of(p).units * 2 * sizeof(int32_t);
+}
 
 hipError_t launch_paged_attention(const Paged& p, hipStream_t stream) {
   PPlan pl = plan_of(p);
   pl.part_o = static_cast<float*>(p.workspace);
   pl.part_ml = pl.part_o + (size_t)groups_of(p) * 2 * kCols * p.d;
+  pl.owners = reinterpret_cast<int32_t*>(pl.part_ml + (size_t)groups_of(p) * 2 * 2 * kCols);
   if (p.dtype == PISA_BF16) return p.d == 64 ? launch_td<__bf16, 64>(p, pl, stream) : launch_td<__bf16, 128>(p, pl, stream);
   return p.d == 64 ? launch_td<float, 64>(p, pl, stream) : launch_td<float, 128>(p, pl, stream);
 }

@@ -58,6 +58,10 @@ template <typename T, int D> __device__ inline int swz(int r) {
 __device__ inline void dma_1kb(unsigned lds, unsigned voff, const unsigned char* base /* both uniform */) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory", "m0");
 }
+// The same for one 4-byte word a lane.
+__device__ inline void dma_words(unsigned lds, unsigned voff, const void* base /* uniform, as lds */) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory", "m0");
+}
 __device__ inline void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }     // vmcnt(0), the other counters left alone
 
 // This lane's part in loading tiles of a tensor with `stride` bytes from row to row.

@@ -113,8 +113,7 @@ def test_zero_keys(lib, dtype):
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp32", 64)])
 def test_few_rows_and_many_keys_are_shared_out(lib, dtype, d):
     q, k, v, dout = make(4, 1, 2, 1, 3, 2500, d, dtype)
-    shape = lib._masked_shape(q, k, v, q, True, None, 0.0, None)
-    assert lib.raw().pisa_masked_attention_workspace_bytes(shape) > 0
+    assert lib.masked_attention_workspace_bytes(q, k, v, causal=True) > 0
     check(lib, q, k, v, dout, True, None, None)
     check(lib, q, k, v, dout, True, [[0, 2499, 2500]], None)      # rows that see one key, in the last part alone
 
@@ -243,9 +242,8 @@ def test_graph_replays_match_eager_calls(lib):
     docs = ints([[0, 200, 320]])
     out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device=DEV)
     dq, dk, dv = (torch.empty_like(x) for x in (q, k, v))
-    shape = lib._masked_shape(q, k, v, out, True, docs, 0.0, None)
-    ws = torch.empty(max(lib.raw().pisa_masked_attention_workspace_bytes(shape),
-                         lib.raw().pisa_masked_attention_backward_workspace_bytes(shape)), dtype=torch.uint8, device=DEV)
+    ws = torch.empty(max(lib.masked_attention_workspace_bytes(q, k, v, True, docs, backward=x) for x in (False, True)),
+                     dtype=torch.uint8, device=DEV)
 
     def step():
         lib.masked_attention(q, k, v, causal=True, doc_offsets=docs, out=out, lse=lse, workspace=ws)

@@ -248,8 +248,7 @@ def test_graph_replays_follow_the_lengths(lib):
     kn, vn = (torch.randn(2, kvh, d, generator=g).to(torch.bfloat16).to(DEV) for _ in range(2))
     one = torch.arange(3, dtype=torch.int32, device=DEV)
     out, lse = torch.empty_like(q), torch.empty(2, h, device=DEV)
-    shape = lib._paged_shape(kp, vp, table, h, 0.0, None)
-    ws = torch.empty(lib.raw().pisa_paged_attention_workspace_bytes(shape), dtype=torch.uint8, device=DEV)
+    ws = torch.empty(lib.paged_attention_workspace_bytes(q, kp, vp, table), dtype=torch.uint8, device=DEV)
 
     def step():
         lib.paged_append(kn, vn, one, kp, vp, table, lengths)
