@@ -31,6 +31,8 @@ size_t masked_workspace_bytes(const Masked& m);
 hipError_t launch_masked_attention(const Masked& m, hipStream_t stream);
 size_t masked_backward_workspace_bytes(const Masked& m);
 hipError_t launch_masked_backward(const Masked& m, hipStream_t stream);
+hipError_t launch_masked_attention_f32(const Masked& m, hipStream_t stream);
+hipError_t launch_masked_backward_f32(const Masked& m, hipStream_t stream);
 
 // Keys (of a row) or rows (of a key): lo <= x < hi; empty where lo >= hi.
 struct Interval {

@@ -7,6 +7,8 @@
 //     dk, dv walk (a lane holds one key):    S = Q K^T,    dP = dO V^T,    dV^T += dO^T P,  dK^T += Q^T dS
 // so that P and dS leave the first products in the lanes in which the second ones take them.  The dk, dv walk goes over the
 // rows of all query heads that share the key head.
+#include <algorithm>
+
 #include "masked.h"
 #include "tile.h"
 
@@ -18,13 +20,13 @@ namespace {
 
 constexpr int kOwn = 128;                // rows (keys) of a workgroup, 32 to a wave
 constexpr int CAP = 1, BIAS = 2;         // bits of MOD
-constexpr float kHeavy = 0.25f;        // see masked_dq_kernel
-constexpr int kHeavyBits = 12;           // of a walk's tiles, 4 096 are told apart
+constexpr float kHeavy = 0.1875f;        // see masked_dq_kernel
+constexpr int kMostHeavy = 5;            // weights of a row that can be as large
 
 struct Plan {
   Deal deal;           // of tiles of 128 rows (dq), or keys (dk, dv) and the parts of their rows
   float* stat;         // [-lse, delta][batch][heads][q_len], the first in the domain of the scores
-  float* part;         // parts > 1: [head][tile][part][dk, dv][128][d]
+  float* part;         // parts > 1: [head][tile][part][dk, dv][128][d]; dq: [head][tile][part][128][d]
 };
 
 // Nothing is moved across, where registers are short.
@@ -42,18 +44,17 @@ template <typename T, int MOD> struct Scorer {
     cap = p.cap * u;
     slope = MOD & BIAS ? p.slopes[head] * u : 0.f;
   }
-  // the weight exp(z - lse) of the raw product s; `far` = |pos - key|; *gain = dz/ds
+  // raw products to what weight() takes: capped ones to their tanh
+  __device__ inline void prepare(f32x16& s) const {
+    if (MOD & CAP) cap_scores<T>(s, to_cap, 1.f);
+  }
+  // the weight exp(z - lse); `far` = |pos - key|; *gain = dz/ds
   __device__ inline float weight(float s, float minus_lse, float far, float* gain) const {
     *gain = 1.f;
     if (!MOD) return exp_diff<T>(s, c, minus_lse);
-    float z = s * to_cap;
-    if (MOD & CAP) {
-      const float t = tanh_of<T>(z);
-      *gain = (1.f - t) * (1.f + t);
-      z = cap * t;
-    }
-    if (MOD & BIAS) z = fmaf(-slope, far, z);
-    return exp_diff<T>(z, 1.f, minus_lse);
+    if (MOD & CAP) *gain = (1.f - s) * (1.f + s);
+    const float z = s * (MOD & CAP ? cap : to_cap);
+    return exp_diff<T>(MOD & BIAS ? fmaf(-slope, far, z) : z, 1.f, minus_lse);
   }
 };
 template <typename T> __device__ inline float in_domain(float lse) { return sizeof(T) == 2 ? lse * kLog2e : lse; }
@@ -109,12 +110,15 @@ template <typename T, int D, int MOD>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(Masked p, Plan plan) {
   using G = Geo<T, D>;
   constexpr int TILEB = G::TILEB, NDT = G::NDT;
-  constexpr bool TIGHT = sizeof(T) == 2 && D == 128;
+  constexpr bool TIGHT = sizeof(T) == 2 && D == 128, ANEW = TIGHT || sizeof(T) == 4;
   __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * TILEB];      // K0 | V0 | K1 | V1
   constexpr bool MENDS = sizeof(T) == 2;
   __shared__ int span_s[4][4];
   __shared__ unsigned bad[2];
-  __shared__ unsigned heavy[MENDS ? (1 << kHeavyBits) / 32 : 1];       // tiles of this walk (or runs of them) with large weights
+  __shared__ struct {
+    int key;
+    float weight;                                // times dz/ds
+  } heavy[MENDS ? kMostHeavy : 1][MENDS ? 256 : 1];      // by thread: of its row, keys with its h
 
   __shared__ int32_t docs_s[kDocsInLds + 1];
   __shared__ int size_s[kRankedTiles + 1];
@@ -132,19 +136,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
   const bool sees = iv.lo < iv.hi;
   const Span ws = span_of_wave(iv);
   if (tid < 2) bad[tid] = 0u;
-  if (MENDS)
-    for (int i = tid; i < (1 << kHeavyBits) / 32; i += 256) heavy[i] = 0u;
   const Span gs = span_of_group(ws, span_s, wave, lane);
 
   const unsigned char* kg = p.k + b * p.sk.batch + (head / p.group) * p.sk.head;
   const unsigned char* vg = p.v + b * p.sv.batch + (head / p.group) * p.sv.head;
   const unsigned lds = (unsigned)(unsigned long long)(LDS_PTR(unsigned char)) & stage[0];
-  Loader<T, D> lk, lv;
+  Loader<T, D, ANEW> lk, lv;
   lk.init(wave, lane, (unsigned)p.sk.token);
   lv.init(wave, lane, (unsigned)p.sv.token);
   Reader<T, D> rd;
   rd.init(lane, lds);
-  auto load = [&](int t, int par) {
+  auto load = [&](int t, int par) INLINE {
     lk.load(wave, lane, kg + (long long)t * kRows * p.sk.token, p.kv_len - t * kRows, lds + 2 * par * TILEB);
     lv.load(wave, lane, vg + (long long)t * kRows * p.sv.token, p.kv_len - t * kRows, lds + (2 * par + 1) * TILEB);
   };
@@ -152,8 +154,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
   if (gs.lo < gs.hi) {
     t_begin = gs.lo / kRows;
     t_end = (gs.hi + kRows - 1) / kRows;
-    load(t_begin, 0);
   }
+  if (!MENDS && plan.deal.n_parts > 1) {
+    const int n = t_end - t_begin, first = t_begin;
+    t_begin = first + (int)((long long)n * share.part / plan.deal.n_parts);
+    t_end = first + (int)((long long)n * (share.part + 1) / plan.deal.n_parts);
+  }
+  if (t_begin < t_end) load(t_begin, 0);
 
   u32x4 q[G::STEPS], g[G::STEPS];                // the lane's rows of q and dout; zeros where the row sees nothing
   float delta = 0.f, minus_lse = 0.f;
@@ -180,14 +187,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
 #pragma unroll
   for (int dt = 0; dt < NDT; ++dt) acc[dt] = (f32x16){0};
   // bf16: delta from a rounded out is off by e = -sum_j dz_ij (the sum is 0 otherwise), and dq by -e sum_j p_ij k_j, which is
-  // as much as the other roundings together where few keys have most of a row's weight.  e is known when the walk is done;
-  // the tiles with weights of kHeavy and more are then walked once more for that sum (below kHeavy the rest does not
-  // matter: the sum falls with the number of keys that share the weight, and so does e).
+  // as much as the other roundings together where few keys have most of a row's weight.  e is known when the walk is done; the
+  // part of that sum that weights of kHeavy and more have, of which a row has few, is taken out then.  (The others' does not
+  // matter: the sum falls with the number of keys that share the weight, and so does e.)
   float off = 0.f;
-  const int heavy_shift = MENDS ? max(0, 32 - __builtin_clz(max(t_end - t_begin, 1) - 1 | 1) - kHeavyBits) : 0;
+  int n_heavy = 0;
 
-  for (int t = t_begin; t < t_end; ++t) {
-    const int par = (t - t_begin) & 1;
+  auto trip = [&](int t, auto parity) INLINE {
+    const int par = parity;
     const unsigned k_off = 2 * par * TILEB, v_off = k_off + TILEB;
     wait_loads();
     __syncthreads();
@@ -196,19 +203,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
       clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0] + k_off, (LDS_PTR(unsigned))&bad[0], tid);
       __syncthreads();
     }
-    if (!touches(ws, t * kRows, kRows)) continue;
+    if (!touches(ws, t * kRows, kRows)) return;
     const bool part = !covers(ws, t * kRows, kRows);
-    float top = 0.f;
-    auto half = [&](auto row0_tag) {
+    auto half = [&](auto row0_tag) INLINE {
       constexpr int ROW0 = decltype(row0_tag)::value;
       int lo = iv.lo;                            // addresses and key numbers are made anew, see masked_dkv_kernel
-      if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols[0]), "+v"(rd.cols[1]), "+v"(lo));
-      const f32x16 s = rows_times<T, D, ROW0>(rd, k_off, q);
+      if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols), "+v"(lo));
+      f32x16 s = rows_times<T, D, ROW0>(rd, k_off, q);
+      sc.prepare(s);
       const f32x16 dp = rows_times<T, D, ROW0>(rd, v_off, g);
       phase<TIGHT>();
       Weights<T> w;
       const unsigned n = (unsigned)(iv.hi - iv.lo);
       const int key0 = t * kRows + ROW0 + 4 * h;
+      float top = 0.f;
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
         float x[2];
@@ -227,72 +235,60 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
         }
         w.set(r, x[0], x[1]);
       }
+      if (MENDS && __builtin_expect(__any(top >= kHeavy), 0)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = key0 + (r / 4) * 8 + r % 4;
+          float gain;
+          const float wt = sc.weight(s[r], minus_lse, fabsf((float)(pos - key)), &gain);
+          if (wt >= kHeavy && (unsigned)(key - lo) < n && n_heavy < kMostHeavy) {
+            heavy[n_heavy][tid].key = key;
+            heavy[n_heavy][tid].weight = wt * gain;
+            ++n_heavy;
+          }
+        }
+      }
       phase<TIGHT>();
       cols_times<T, D, ROW0>(rd, k_off, w, acc);
     };
     half(std::integral_constant<int, 0>{});
     phase<TIGHT>();
     half(std::integral_constant<int, 32>{});
-    if (MENDS && __any(top >= kHeavy) && lane == 0) {
-      const int at = (t - t_begin) >> heavy_shift;
-      atomicOr(&heavy[at >> 5], 1u << (at & 31));
-    }
-  }
+  };
+  walk_stages<T>(t_begin, t_end, trip);
   if constexpr (MENDS) {
     off += __shfl_xor(off, 32);
     delta += off;
-    __syncthreads();
-    for (int t = t_begin; t < t_end; ++t) {
-      const int at = (t - t_begin) >> heavy_shift;
-      const unsigned word = __builtin_amdgcn_readfirstlane(heavy[at >> 5]);
-      if (!(word >> (at & 31) & 1u)) {           // uniform over the workgroup
-        if (word == 0u && heavy_shift == 0) t += 31 - (at & 31);
-        continue;
-      }
-      __syncthreads();                           // the tile before has been read
-      lk.load(wave, lane, kg + (long long)t * kRows * p.sk.token, p.kv_len - t * kRows, lds);
-      wait_loads();
-      __syncthreads();
-      if (!covers(gs, t * kRows, kRows)) {
-        clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0], (LDS_PTR(unsigned))&bad[0], tid);
-        __syncthreads();
-      }
-      if (!touches(ws, t * kRows, kRows)) continue;
-      const bool part = !covers(ws, t * kRows, kRows);
-      auto half = [&](auto row0_tag) {
-        constexpr int ROW0 = decltype(row0_tag)::value;
-        int lo = iv.lo;
-        if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols[0]), "+v"(rd.cols[1]), "+v"(lo));
-        const f32x16 s = rows_times<T, D, ROW0>(rd, 0, q);
-        phase<TIGHT>();
-        Weights<T> w;
-        const unsigned n = (unsigned)(iv.hi - iv.lo);
-        const int key0 = t * kRows + ROW0 + 4 * h;
+    const int others = __shfl_xor(n_heavy, 32);
+    const int counts[2] = {h ? others : n_heavy, h ? n_heavy : others};
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          float x[2];
+    for (int half = 0; half < 2; ++half)         // the row's keys of h = 0, then of h = 1, by either lane for its channels
+      for (int e = 0; __any(e < counts[half]); ++e)
+        if (e < counts[half]) {
+          const int of = (tid & ~32) + 32 * half;
+          const T* src = reinterpret_cast<const T*>(kg + (long long)heavy[e][of].key * p.sk.token);
+          const float f = -off * heavy[e][of].weight;
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const int key = key0 + ((r + u) / 4) * 8 + (r + u) % 4;
-            float gain;
-            x[u] = -off * sc.weight(s[r + u], minus_lse, fabsf((float)(pos - key)), &gain);
-            if (MOD & CAP) x[u] *= gain;
-            if (part && (unsigned)(key - lo) >= n) x[u] = 0.f;
-          }
-          w.set(r, x[0], x[1]);
+          for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              const u32x2 x = *reinterpret_cast<const u32x2*>(src + 32 * dt + 8 * g + 4 * h);
+              acc[dt][4 * g] = fmaf(f, __uint_as_float(x.x << 16), acc[dt][4 * g]);
+              acc[dt][4 * g + 1] = fmaf(f, __uint_as_float(x.x & 0xffff0000u), acc[dt][4 * g + 1]);
+              acc[dt][4 * g + 2] = fmaf(f, __uint_as_float(x.y << 16), acc[dt][4 * g + 2]);
+              acc[dt][4 * g + 3] = fmaf(f, __uint_as_float(x.y & 0xffff0000u), acc[dt][4 * g + 3]);
+            }
         }
-        phase<TIGHT>();
-        cols_times<T, D, ROW0>(rd, 0, w, acc);
-      };
-      half(std::integral_constant<int, 0>{});
-      phase<TIGHT>();
-      half(std::integral_constant<int, 32>{});
-    }
   }
-  if (row < p.q_len && h == 0) {
+  if (row < p.q_len && h == 0 && share.part == 0) {
     float* st = plan.stat + (size_t)bh * p.q_len + row;
     st[0] = minus_lse;
     st[(size_t)p.batch * p.heads * p.q_len] = sees ? delta : 0.f;
+  }
+  if (!MENDS && plan.deal.n_parts > 1) {
+    const size_t item = ((size_t)bh * plan.deal.n_tiles + qt) * plan.deal.n_parts + share.part;
+    store_row<float, D>(reinterpret_cast<unsigned char*>(plan.part + (item * kOwn + 32 * wave + lam) * D), acc, p.scale, sees, h);
+    return;
   }
   if (row < p.q_len)
     store_row<T, D>(p.dq + b * p.sdq.batch + head * p.sdq.head + (long long)row * p.sdq.token, acc, p.scale, sees, h);
@@ -302,9 +298,10 @@ template <typename T, int D, int MOD>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel(Masked p, Plan plan) {
   using G = Geo<T, D>;
   constexpr int TILEB = G::TILEB, NDT = G::NDT;
-  constexpr bool TIGHT = sizeof(T) == 2 && D == 128;
+  constexpr bool TIGHT = sizeof(T) == 2 && D == 128, ANEW = TIGHT || sizeof(T) == 4;
   __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * TILEB];      // Q0 | dO0 | Q1 | dO1
   __shared__ __attribute__((aligned(16))) float stat[2][2][kRows];               // [parity][-lse, delta][row]
+  __shared__ Interval seen_s[kOwn];              // for the tiles that need it: no registers for it in the walk
   __shared__ int span_s[4][4];
   __shared__ unsigned bad[2];
 
@@ -322,13 +319,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel
   Interval iv{0, 0};
   if (key < p.kv_len) iv = rows_of_key(p, offs, b, key);
   const bool seen = iv.lo < iv.hi;
+  seen_s[32 * wave + lam] = iv;
   const Span ws = span_of_wave(iv);
   if (tid < 2) bad[tid] = 0u;
   const Span gs = span_of_group(ws, span_s, wave, lane);
 
   const unsigned lds = (unsigned)(unsigned long long)(LDS_PTR(unsigned char)) & stage[0];
   const unsigned lds_stat = (unsigned)(unsigned long long)(LDS_PTR(float)) & stat[0][0][0];
-  Loader<T, D> lq, lg;
+  Loader<T, D, ANEW> lq, lg;
   lq.init(wave, lane, (unsigned)p.sq.token);
   lg.init(wave, lane, (unsigned)p.sdo.token);
   Reader<T, D> rd;
@@ -348,11 +346,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel
     t += i_begin % n;
   }
   const size_t all_rows = (size_t)p.batch * p.heads * p.q_len;
-  auto load = [&](int par) {
+  auto load = [&](int par) INLINE {
     const int avail = p.q_len - t * kRows;
     if (wave < 2) {
       const float* st = plan.stat + wave * all_rows + ((size_t)b * p.heads + head) * p.q_len + t * kRows;
-      dma_words(lds_stat + (par * 2 + wave) * (kRows * 4), (unsigned)(min(lane, avail - 1) * 4), st);
+      dma_words(lds_stat + (par * 2 + wave) * (kRows * 4), (unsigned)(min(TIGHT ? lane_anew() : lane, avail - 1) * 4), st);
     }
     lq.load(wave, lane, p.q + b * p.sq.batch + head * p.sq.head + (long long)t * kRows * p.sq.token, avail, lds + 2 * par * TILEB);
     lg.load(wave, lane, p.dout + b * p.sdo.batch + head * p.sdo.head + (long long)t * kRows * p.sdo.token, avail,
@@ -378,8 +376,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel
 
   if (i_begin < i_end) load(0);
   const int shift = p.kv_len - p.q_len;
-  for (int i = i_begin; i < i_end; ++i) {
-    const int par = (i - i_begin) & 1;
+  auto trip = [&](int i, auto parity) INLINE {
+    const int par = parity;
     const unsigned q_off = 2 * par * TILEB, g_off = q_off + TILEB;
     const int x0 = t * kRows, head_now = head;
     wait_loads();
@@ -392,25 +390,32 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel
       load(par ^ 1);
     }
     if (!covers(gs, x0, kRows)) {         // both second products contract over rows that do not all see every key
-      clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0] + q_off, (LDS_PTR(unsigned))&bad[0], tid);
-      clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0] + g_off, (LDS_PTR(unsigned))&bad[0], tid);
+      const int thread = TIGHT ? 64 * wave + lane_anew() : tid;
+      clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0] + q_off, (LDS_PTR(unsigned))&bad[0], thread);
+      clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0] + g_off, (LDS_PTR(unsigned))&bad[0], thread);
       __syncthreads();
     }
-    if (!touches(ws, x0, kRows)) continue;
+    if (!touches(ws, x0, kRows)) return;
     const bool part = !covers(ws, x0, kRows);
     const Scorer<T, MOD> sc(p, head_now);
-    auto half = [&](auto row0_tag) {
+    auto half = [&](auto row0_tag) INLINE {
       constexpr int ROW0 = decltype(row0_tag)::value;
       // 192 of 256 registers hold k, v, dk and dv: addresses and row numbers are made anew where they are wanted, and the
       // products are kept apart from what follows, or the scheduler spills to feed them early
-      int lo = iv.lo;
-      if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols[0]), "+v"(rd.cols[1]), "+v"(lo));
-      const f32x16 s = rows_times<T, D, ROW0>(rd, q_off, k);
+      if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols));
+      f32x16 s = rows_times<T, D, ROW0>(rd, q_off, k);
+      sc.prepare(s);
       const f32x16 dp = rows_times<T, D, ROW0>(rd, g_off, v);
       phase<TIGHT>();
       Weights<T> wp, wd;
-      const unsigned count = (unsigned)(iv.hi - iv.lo);
-      const int row0 = x0 + ROW0 + 4 * h;
+      const int ln = TIGHT ? lane_anew() : lane, h = ln >> 5, own = 32 * wave + (ln & 31);   // own: this lane's key of the tile
+      int lo = 0;
+      unsigned count = 0u;
+      if (part) {
+        lo = seen_s[own].lo;
+        count = (unsigned)(seen_s[own].hi - lo);
+      }
+      const int row0 = x0 + ROW0 + 4 * h, key = kt * kOwn + own;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const f32x4 ml = *reinterpret_cast<LDS_PTR(const f32x4)>((LDS_PTR(const float))&stat[par][0][ROW0 + 8 * e + 4 * h]);
@@ -440,7 +445,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel
     half(std::integral_constant<int, 0>{});
     phase<TIGHT>();
     half(std::integral_constant<int, 32>{});
-  }
+  };
+  walk_stages<T>(i_begin, i_end, trip);
 
   if (plan.deal.n_parts > 1) {
     const size_t item = ((size_t)bk * plan.deal.n_tiles + kt) * plan.deal.n_parts + share.part;
@@ -455,18 +461,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel
   }
 }
 
-// Adds the parts of a key tile's dk and dv: a thread has four channels of one row of either.
-template <typename T, int D> __global__ __launch_bounds__(256) void masked_dkv_join_kernel(Masked p, Plan plan) {
+// Adds the parts of 128 rows: a thread has four channels of one.  blockIdx.z: which of the tensors that lie side by side.
+struct JoinTo {
+  unsigned char* at[2];
+  Strides stride[2];
+  int heads, len, count;       // count: of those tensors
+};
+template <typename T, int D> __global__ __launch_bounds__(256) void masked_sum_kernel(Plan plan, JoinTo to) {
   constexpr int PER_ROW = D / 4, ROWS = 256 / PER_ROW;
-  const int unit = blockIdx.y, tid = threadIdx.x, which = blockIdx.z;
-  const int bk = unit / plan.deal.n_tiles, b = bk / p.kv_heads, kv_head = bk % p.kv_heads;
-  const int r = blockIdx.x * ROWS + tid / PER_ROW, ch = 4 * (tid % PER_ROW), key = unit % plan.deal.n_tiles * kOwn + r;
-  if (key >= p.kv_len) return;
+  const int unit = blockIdx.y, tid = threadIdx.x, which = blockIdx.z, n_parts = plan.deal.n_parts;
+  const int bh = unit / plan.deal.n_tiles, b = bh / to.heads, head = bh % to.heads;
+  const int r = blockIdx.x * ROWS + tid / PER_ROW, ch = 4 * (tid % PER_ROW), row = unit % plan.deal.n_tiles * kOwn + r;
+  if (row >= to.len) return;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < plan.deal.n_parts; ++i)
-    sum += *reinterpret_cast<const f32x4*>(plan.part + ((((size_t)unit * plan.deal.n_parts + i) * 2 + which) * kOwn + r) * D + ch);
-  const Strides& sd = which ? p.sdv : p.sdk;
-  unsigned char* dst = (which ? p.dv : p.dk) + b * sd.batch + kv_head * sd.head + (long long)key * sd.token;
+  for (int i = 0; i < n_parts; ++i)
+    sum += *reinterpret_cast<const f32x4*>(plan.part + ((((size_t)unit * n_parts + i) * to.count + which) * kOwn + r) * D + ch);
+  const Strides& sd = to.stride[which];
+  unsigned char* dst = to.at[which] + b * sd.batch + head * sd.head + (long long)row * sd.token;
   if constexpr (sizeof(T) == 2)
     *reinterpret_cast<u32x2*>(dst + 2 * ch) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
   else
@@ -474,9 +485,17 @@ template <typename T, int D> __global__ __launch_bounds__(256) void masked_dkv_j
 }
 
 int tiles_of(int n) { return (n + kOwn - 1) / kOwn; }
+long long f32_parts(const Masked& m, long long units) { return ((m.d == 64 ? 512 : 768) + units - 1) / units; }
+int at_least_one(long long parts) { return parts < 1 ? 1 : (int)parts; }
 Plan plan_q(const Masked& m) {
   Plan pl{};
-  pl.deal = deal_of(m.batch * m.heads, tiles_of(m.q_len), 1, m.dtype == PISA_BF16 ? 64 : 32);
+  const long long units = (long long)m.batch * m.heads * tiles_of(m.q_len);
+  const bool f32 = m.dtype == PISA_FP32;
+  // fp32 products take so long that the keys of a tile are shared out until every compute unit has three workgroups to do (two
+  // at 64 channels).  bf16 walks are not: what mends delta needs a row's whole sum.
+  const long long tiles = (m.kv_len + kRows - 1) / kRows;
+  const long long parts = f32 ? std::min(f32_parts(m, units), tiles / 2) : 1;
+  pl.deal = deal_of(m.batch * m.heads, tiles_of(m.q_len), at_least_one(parts), f32 ? 32 : 64);
   return pl;
 }
 Plan plan_kv(const Masked& m) {
@@ -487,22 +506,37 @@ Plan plan_kv(const Masked& m) {
   // us, whole / shared out: 2 x 4 key heads of 2 777, 64 channels, 583 / 259; 13 heads of 6 000, causal, 988 / 845).  Causal
   // tiles differ in size and leave places idle for longer: up to 800 (12 of 8 192 1 112 / 1 018), the others up to 640 (24 of
   // 4 000 in documents, 768 tiles, 323 / 352).
+  const bool f32 = m.dtype == PISA_FP32;
   const long long steps = (long long)m.group * ((m.q_len + kRows - 1) / kRows);
-  long long parts = units >= (m.causal ? 800 : 640) ? 1 : (1024 + units - 1) / units;
-  parts = parts < steps / 4 ? parts : steps / 4;
-  pl.deal = deal_of(m.batch * m.kv_heads, tiles_of(m.kv_len), parts < 1 ? 1 : (int)parts, m.dtype == PISA_BF16 ? 64 : 32);
+  const long long parts = f32 ? std::min(f32_parts(m, units), steps / 2)
+                              : (units >= (m.causal ? 800 : 640) ? 1 : std::min((1024 + units - 1) / units, steps / 4));
+  pl.deal = deal_of(m.batch * m.kv_heads, tiles_of(m.kv_len), at_least_one(parts), f32 ? 32 : 64);
   return pl;
 }
-size_t items_of(const Plan& pl, const Masked& m) { return (size_t)m.batch * m.kv_heads * pl.deal.n_tiles * pl.deal.n_parts; }
+// Floats of the parts' sums: dq's are added up before the dk, dv walk writes its own.
+size_t part_floats(const Masked& m, const Plan& pq, const Plan& pk) {
+  const size_t q = pq.deal.n_parts > 1 ? (size_t)m.batch * m.heads * pq.deal.n_tiles * pq.deal.n_parts * kOwn * m.d : 0;
+  const size_t k = pk.deal.n_parts > 1 ? (size_t)m.batch * m.kv_heads * pk.deal.n_tiles * pk.deal.n_parts * 2 * kOwn * m.d : 0;
+  return std::max(q, k);
+}
 
 template <typename T, int D, int MOD> hipError_t launch_mod(const Masked& m, const Plan& pq, const Plan& pk, hipStream_t stream) {
-  hipLaunchKernelGGL((masked_dq_kernel<T, D, MOD>), dim3(8 * pq.deal.per_xcd), dim3(256), 0, stream, m, pq);
+  const dim3 block(256);
+  const int slices = kOwn / (256 / (D / 4));
+  hipLaunchKernelGGL((masked_dq_kernel<T, D, MOD>), dim3(8 * pq.deal.per_xcd), block, 0, stream, m, pq);
   hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (pq.deal.n_parts > 1) {
+    const JoinTo to{{m.dq, nullptr}, {m.sdq, {}}, m.heads, m.q_len, 1};
+    hipLaunchKernelGGL((masked_sum_kernel<T, D>), dim3(slices, m.batch * m.heads * pq.deal.n_tiles, 1), block, 0, stream, pq, to);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || m.kv_len == 0) return e;
-  hipLaunchKernelGGL((masked_dkv_kernel<T, D, MOD>), dim3(8 * pk.deal.per_xcd), dim3(256), 0, stream, m, pk);
+  hipLaunchKernelGGL((masked_dkv_kernel<T, D, MOD>), dim3(8 * pk.deal.per_xcd), block, 0, stream, m, pk);
   e = hipGetLastError();
   if (e != hipSuccess || pk.deal.n_parts == 1) return e;
-  hipLaunchKernelGGL((masked_dkv_join_kernel<T, D>), dim3(kOwn / (256 / (D / 4)), m.batch * m.kv_heads * pk.deal.n_tiles, 2), dim3(256), 0, stream, m, pk);
+  const JoinTo to{{m.dk, m.dv}, {m.sdk, m.sdv}, m.kv_heads, m.kv_len, 2};
+  hipLaunchKernelGGL((masked_sum_kernel<T, D>), dim3(slices, m.batch * m.kv_heads * pk.deal.n_tiles, 2), block, 0, stream, pk, to);
   return hipGetLastError();
 }
 template <typename T, int D> hipError_t launch_td(const Masked& m, const Plan& pq, const Plan& pk, hipStream_t stream) {
@@ -516,19 +550,33 @@ template <typename T, int D> hipError_t launch_td(const Masked& m, const Plan& p
 
 size_t stat_bytes(const Masked& m) { return (2 * (size_t)m.batch * m.heads * m.q_len * sizeof(float) + 255) & ~(size_t)255; }
 
+void places_in(const Masked& m, Plan* pq, Plan* pk) {          // the plans, with their places in the workspace
+  *pq = plan_q(m);
+  *pk = plan_kv(m);
+  pq->stat = pk->stat = static_cast<float*>(m.workspace);
+  pq->part = pk->part = reinterpret_cast<float*>(static_cast<unsigned char*>(m.workspace) + stat_bytes(m));
+}
+
 }  // namespace
 
+// The fp32 kernels are compiled by themselves, from this file with PISA_MASKED_F32 set (build.py).
+#ifdef PISA_MASKED_F32
+hipError_t launch_masked_backward_f32(const Masked& m, hipStream_t stream) {
+  Plan pq, pk;
+  places_in(m, &pq, &pk);
+  return m.d == 64 ? launch_td<float, 64>(m, pq, pk, stream) : launch_td<float, 128>(m, pq, pk, stream);
+}
+#else
 size_t masked_backward_workspace_bytes(const Masked& m) {
-  const Plan pk = plan_kv(m);
-  return stat_bytes(m) + (pk.deal.n_parts > 1 ? items_of(pk, m) * 2 * kOwn * m.d * sizeof(float) : 0);
+  return stat_bytes(m) + part_floats(m, plan_q(m), plan_kv(m)) * sizeof(float);
 }
 
 hipError_t launch_masked_backward(const Masked& m, hipStream_t stream) {
-  Plan pq = plan_q(m), pk = plan_kv(m);
-  pq.stat = pk.stat = static_cast<float*>(m.workspace);
-  pk.part = reinterpret_cast<float*>(static_cast<unsigned char*>(m.workspace) + stat_bytes(m));
-  if (m.dtype == PISA_BF16) return m.d == 64 ? launch_td<__bf16, 64>(m, pq, pk, stream) : launch_td<__bf16, 128>(m, pq, pk, stream);
-  return m.d == 64 ? launch_td<float, 64>(m, pq, pk, stream) : launch_td<float, 128>(m, pq, pk, stream);
+  if (m.dtype == PISA_FP32) return launch_masked_backward_f32(m, stream);
+  Plan pq, pk;
+  places_in(m, &pq, &pk);
+  return m.d == 64 ? launch_td<__bf16, 64>(m, pq, pk, stream) : launch_td<__bf16, 128>(m, pq, pk, stream);
 }
+#endif
 
 }  // namespace pisa

@@ -6,6 +6,8 @@
 // each for K and V, one barrier a tile: behind it the loads of K(t+2) and V(t+1) go out, then the softmax of tile t,
 // O^T += V(t)^T P(t)^T and S^T(t+1).  The walk goes over the tiles that some row of the workgroup sees; a wave leaves out
 // those that none of its rows sees, and compares key numbers only in those that some of them see in part.
+#include <algorithm>
+
 #include "masked.h"
 #include "tile.h"
 
@@ -139,32 +141,32 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
     t_end = first + (int)((long long)n * (share.part + 1) / plan.deal.n_parts);
   }
 
-  auto load_k = [&](int t, int stage_at) {
+  auto load_k = [&](int t, int stage_at) INLINE {
     lk.load(wave, lane, kg + (long long)t * kRows * p.sk.token, p.kv_len - t * kRows, lds + stage_at * TILEB);
   };
-  auto load_v = [&](int t, int stage_at) {
+  auto load_v = [&](int t, int stage_at) INLINE {
     lv.load(wave, lane, vg + (long long)t * kRows * p.sv.token, p.kv_len - t * kRows, lds + (2 + stage_at) * TILEB);
   };
   f32x16 s0, s1;                                 // S^T of the tile at hand: keys 0..31, 32..63
-  auto scores = [&](int t, unsigned off) {
+  auto scores = [&](int t, unsigned off) INLINE {
     if (!touches(ws, t * kRows, kRows)) return;
     s0 = rows_times<T, D, 0>(rd, off, q);
     s1 = rows_times<T, D, 32>(rd, off, q);
-    if (MOD) {
+    if (MOD & CAP) {
+      cap_scores<T>(s0, to_cap, cap);
+      cap_scores<T>(s1, to_cap, cap);
+    }
+    if (MOD & BIAS) {
+      const int ahead = pos - t * kRows - 4 * h;   // of key 0 of this lane's
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int key = t * kRows + (r / 4) * 8 + 4 * h + r % 4;
-        float x = s0[r] * to_cap, y = s1[r] * to_cap;
-        if (MOD & CAP) {
-          x = cap * tanh_of<T>(x);
-          y = cap * tanh_of<T>(y);
+        const int key = (r / 4) * 8 + r % 4;
+        if (!(MOD & CAP)) {
+          s0[r] *= to_cap;
+          s1[r] *= to_cap;
         }
-        if (MOD & BIAS) {
-          x = fmaf(-slope, fabsf((float)(pos - key)), x);
-          y = fmaf(-slope, fabsf((float)(pos - key - 32)), y);
-        }
-        s0[r] = x;
-        s1[r] = y;
+        s0[r] = fmaf(-slope, fabsf((float)(ahead - key)), s0[r]);
+        s1[r] = fmaf(-slope, fabsf((float)(ahead - key - 32)), s1[r]);
       }
     }
   };
@@ -177,8 +179,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
     load_v(t_begin, 0);
     scores(t_begin, 0);
   }
-  for (int t = t_begin; t < t_end; ++t) {
-    const int par = (t - t_begin) & 1;
+  auto trip = [&](int t, auto parity) INLINE {
+    const int par = parity;
     const unsigned v_off = (2 + par) * TILEB;
     wait_loads();
     __syncthreads();
@@ -247,7 +249,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
       }
     }
     if (t + 1 < t_end) scores(t + 1, (par ^ 1) * TILEB);
-  }
+  };
+  walk_stages<T>(t_begin, t_end, trip);
 
   st.l += __shfl_xor(st.l, 32);
   if (plan.deal.n_parts > 1) {
@@ -316,19 +319,48 @@ template <typename T, int D> __global__ __launch_bounds__(256) void masked_join_
   if (p.lse && ch == 0) p.lse[(size_t)bh * p.q_len + row] = sees ? log_sum<T>(m, l) : -INFINITY;
 }
 
+// Workgroups that share a tile's keys, where the tiles alone leave places on the card idle (64 an XCD in bf16, 32 in fp32) and
+// there are keys enough to share.
 int parts_of(const Masked& m) {
-  const long long units = (long long)m.batch * m.heads * ((m.q_len + kQRows - 1) / kQRows);
-  // Keys are shared out where the tiles alone leave compute units idle and there are keys enough to share.
-  const long long slots = m.dtype == PISA_BF16 ? 512 : 256;
-  const int tiles = (m.kv_len + kRows - 1) / kRows;
-  long long parts = units >= slots ? 1 : slots / units;
-  parts = parts < tiles / 4 ? parts : tiles / 4;
+  const long long units = (long long)m.batch * m.heads * ((m.q_len + kQRows - 1) / kQRows), u = (units + 7) / 8;
+  const long long tiles = (m.kv_len + kRows - 1) / kRows;
+  const bool triangle = m.causal && 2LL * m.q_len > m.kv_len;        // tiles of very different size
+  long long parts = 1;
+  if (m.dtype == PISA_BF16) {
+    // Equal tiles: one round of workgroups, never a few more (24 heads of 500 rows, 9 001 keys, five parts 99 us, six 134).
+    // Those of a triangle are half as long on average and fill places as they end (12 heads of 2 048 two parts 48, three 42,
+    // six 53; 24 of 2 000 one 63, two 56; 13 of 6 000 one 174, two 164).
+    parts = triangle ? (256 + 3 * u - 1) / (3 * u) : 64 / u;
+    parts = std::min(parts, tiles / 4);
+  } else if (triangle) {
+    // fp32 products take so long that three workgroups a compute unit pay (8 heads of 4 500: one part 850, two 574, three
+    // 561, six 586), two at 64 channels.
+    parts = std::min(((m.d == 64 ? 64 : 96) + u - 1) / u, tiles / 2);
+  } else {
+    // whole rounds of the 32 compute units of an XCD, and about a tile's time for a part's own sums and its part in the joining
+    long long best = 1LL << 60;
+    for (long long n = 1; n <= 16 && (n == 1 || n <= tiles / 2); ++n) {
+      const long long rounds = (u * n + 31) / 32, cost = rounds * (tiles * 64 / n + 64);
+      if (cost < best) {
+        best = cost;
+        parts = n;
+      }
+    }
+  }
   return parts < 1 ? 1 : (int)parts;
 }
 size_t items_of(const Plan& pl, const Masked& m) { return (size_t)m.batch * m.heads * pl.deal.n_tiles * pl.deal.n_parts; }
 Plan plan_of(const Masked& m) {
   Plan pl{};
   pl.deal = deal_of(m.batch * m.heads, (m.q_len + kQRows - 1) / kQRows, parts_of(m), m.dtype == PISA_BF16 ? 64 : 32);
+  return pl;
+}
+Plan plan_in(const Masked& m) {                  // with its places in the workspace
+  Plan pl = plan_of(m);
+  if (pl.deal.n_parts > 1) {
+    pl.part_o = static_cast<float*>(m.workspace);
+    pl.part_ml = pl.part_o + items_of(pl, m) * kQRows * m.d;
+  }
   return pl;
 }
 
@@ -348,19 +380,23 @@ template <typename T, int D> hipError_t launch_td(const Masked& m, const Plan& p
 
 }  // namespace
 
+// The fp32 kernels are compiled by themselves, from this file with PISA_MASKED_F32 set (build.py).
+#ifdef PISA_MASKED_F32
+hipError_t launch_masked_attention_f32(const Masked& m, hipStream_t stream) {
+  const Plan pl = plan_in(m);
+  return m.d == 64 ? launch_td<float, 64>(m, pl, stream) : launch_td<float, 128>(m, pl, stream);
+}
+#else
 size_t masked_workspace_bytes(const Masked& m) {
   const Plan pl = plan_of(m);
   return pl.deal.n_parts == 1 ? 0 : items_of(pl, m) * kQRows * (m.d + 2) * sizeof(float);
 }
 
 hipError_t launch_masked_attention(const Masked& m, hipStream_t stream) {
-  Plan pl = plan_of(m);
-  if (pl.deal.n_parts > 1) {
-    pl.part_o = static_cast<float*>(m.workspace);
-    pl.part_ml = pl.part_o + items_of(pl, m) * kQRows * m.d;
-  }
-  if (m.dtype == PISA_BF16) return m.d == 64 ? launch_td<__bf16, 64>(m, pl, stream) : launch_td<__bf16, 128>(m, pl, stream);
-  return m.d == 64 ? launch_td<float, 64>(m, pl, stream) : launch_td<float, 128>(m, pl, stream);
+  if (m.dtype == PISA_FP32) return launch_masked_attention_f32(m, stream);
+  const Plan pl = plan_in(m);
+  return m.d == 64 ? launch_td<__bf16, 64>(m, pl, stream) : launch_td<__bf16, 128>(m, pl, stream);
 }
+#endif
 
 }  // namespace pisa

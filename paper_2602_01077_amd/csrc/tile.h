@@ -27,10 +27,19 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
+// for lambdas that hold a wave's registers by reference: called out of line, those would lie in memory
+#define INLINE __attribute__((always_inline))
 #define LDS_PTR(T) __attribute__((address_space(3))) T*
 
 constexpr int kRows = 64;                        // rows of a staged tile
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// The lane number, made anew where it stands: for loops that have no register to keep it in.
+__device__ inline int lane_anew() {
+  int lane;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+  return lane;
+}
 
 template <typename T, int D> struct Geo {
   static constexpr int ROWB = D * (int)sizeof(T);
@@ -46,7 +55,7 @@ template <typename T, int D> struct Geo {
 // ds_read_b128 of one chunk takes 16 rows on 16 different 16-byte columns of the 64 banks, and the two 16-lane groups of a
 // half-wave that read 32 bytes each of four consecutive rows get eight different 32-byte columns.  fp32: rows r and r + 4,
 // which the two halves read together, lie in different halves of the banks.
-template <typename T, int D> __device__ inline int swz(int r) {
+template <typename T, int D> __host__ __device__ constexpr int swz(int r) {
   if (sizeof(T) == 4) return (((r >> 2) & 1) << 3) | ((r & 3) << 1) | ((r >> 3) & 1);
   if (D == 128) return ((((r & 3) << 1) | ((r >> 2) & 1)) << 1) | ((r >> 3) & 1);
   return (((r >> 1) & 1) << 2) | (((r >> 2) & 1) << 1) | ((r >> 3) & 1);       // two rows share the 64 banks
@@ -64,25 +73,38 @@ __device__ inline void dma_words(unsigned lds, unsigned voff, const void* base /
 }
 __device__ inline void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }     // vmcnt(0), the other counters left alone
 
-// This lane's part in loading tiles of a tensor with `stride` bytes from row to row.
-template <typename T, int D> struct Loader {
+// A wave's part in loading tiles of a tensor with `stride` bytes from row to row: rows 16 wave .. + 15, piece i of them rows
+// RPL i .. + RPL - 1.  Rows past `avail` (>= 1) are replaced by the last valid one; the caller masks them.
+// ANEW: every address is made anew for every tile, from the lane number alone.  The dk, dv walk has no registers for offsets:
+// spilled, their reloads waited between the loads (24 heads of 4 608, backward 1 200 us, so 990).  Elsewhere they are worth
+// a register for each piece (forward 275 us made anew, 257 so).
+template <typename T, int D, bool ANEW = false> struct Loader {
   using G = Geo<T, D>;
-  unsigned off[G::NLD];                          // byte offset from the tile's first row, piece by piece
+  static_assert(G::RPL * G::NLD == 16, "a wave loads 16 rows, the swizzle's period");
   unsigned stride;
+  unsigned off[ANEW ? 1 : G::NLD];               // byte offset from the tile's first row, piece by piece
   __device__ inline static int row(int wave, int lane, int i) { return G::RPL * (G::NLD * wave + i) + lane / G::CPR; }
   __device__ inline static unsigned chunk(int lane, int r) { return (unsigned)(((lane % G::CPR) ^ swz<T, D>(r)) << 4); }
   __device__ inline void init(int wave, int lane, unsigned stride_) {
     stride = stride_;
 #pragma unroll
-    for (int i = 0; i < G::NLD; ++i) {
-      const int r = row(wave, lane, i);
-      off[i] = (unsigned)r * stride + chunk(lane, r);
-    }
+    for (int i = 0; i < (ANEW ? 0 : G::NLD); ++i) off[i] = (unsigned)row(wave, lane, i) * stride + chunk(lane, row(wave, lane, i));
   }
-  // Rows past `avail` (>= 1) are replaced by the last valid one; the caller masks them.
   __device__ inline void load(int wave, int lane, const unsigned char* base, int avail, unsigned lds) const {
     const unsigned at = __builtin_amdgcn_readfirstlane(lds + wave * (G::NLD * 1024));
-    if (avail >= kRows) {
+    if constexpr (ANEW) {
+      lane = lane_anew();
+      const int l = lane / G::CPR;
+      const unsigned chunk0 = chunk(lane, l);
+#pragma unroll
+      for (int i = 0; i < G::NLD; ++i) {
+        // the swizzle only moves bits of the row: that of a row is that of its place in the piece XOR that of the piece
+        const int r0 = 16 * wave + G::RPL * i;
+        const unsigned c = chunk0 ^ (unsigned)(swz<T, D>(G::RPL * i) << 4);
+        if (avail >= kRows) dma_1kb(at + i * 1024, (unsigned)l * stride + c, base + (unsigned)r0 * (unsigned long long)stride);
+        else dma_1kb(at + i * 1024, (unsigned)min(r0 + l, avail - 1) * stride + c, base);
+      }
+    } else if (avail >= kRows) {
 #pragma unroll
       for (int i = 0; i < G::NLD; ++i) dma_1kb(at + i * 1024, off[i], base);
     } else {
@@ -99,19 +121,17 @@ template <typename T, int D> struct Loader {
 template <typename T, int D> struct Reader {
   using G = Geo<T, D>;
   unsigned rows;                                 // 16 bytes of row lam, contraction step 0
-  unsigned cols[2];                              // bf16: columns, rows 0-7 and 8-15 of a contraction step of 16; fp32: rows e and e + 8
+  unsigned cols;                                 // columns: bf16, rows 0..7 of a contraction step of 16 (8..15: bit 4 flips)
   __device__ inline void init(int lane, unsigned tile) {
     const int lam = lane & 31, h = lane >> 5;
     rows = tile + lam * G::ROWB + ((h ^ swz<T, D>(lam)) << 4);
     if (sizeof(T) == 2) {
       // lane j of a 16-lane group points at 4 channels of row j / 4 and receives channel j of the group's four rows
       const int j = lane & 15, kq = 4 * h + (j >> 2), lhalf = (lane >> 4) & 1;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        cols[u] = tile + (kq + 8 * u) * G::ROWB + (((2 * lhalf + ((j & 3) >> 1)) ^ swz<T, D>(kq + 8 * u)) << 4) + 8 * (j & 1);
+      static_assert(sizeof(T) == 4 || swz<T, D>(8) == 1, "row r + 8 lies at row r's chunk XOR 1");
+      cols = tile + kq * G::ROWB + (((2 * lhalf + ((j & 3) >> 1)) ^ swz<T, D>(kq)) << 4) + 8 * (j & 1);
     } else {
-      cols[0] = tile + 4 * h * G::ROWB + (lam & 3) * 4;
-      cols[1] = (unsigned)(lam >> 2);
+      cols = tile + 4 * h * G::ROWB + (lam & 3) * 4;
     }
   }
 };
@@ -173,23 +193,23 @@ __device__ inline void cols_times(const Reader<T, D>& rd, unsigned off, const We
       for (int dt = 0; dt < Geo<T, D>::NDT; ++dt) {
         const unsigned at = off + (ROW0 + 16 * s) * ROWB;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            reinterpret_cast<LDS_PTR(s16x4)>((LDS_PTR(unsigned char))(unsigned long long)((rd.cols[0] ^ (dt << 6)) + at)));
+            reinterpret_cast<LDS_PTR(s16x4)>((LDS_PTR(unsigned char))(unsigned long long)((rd.cols ^ (dt << 6)) + at)));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            reinterpret_cast<LDS_PTR(s16x4)>((LDS_PTR(unsigned char))(unsigned long long)((rd.cols[1] ^ (dt << 6)) + at)));
+            reinterpret_cast<LDS_PTR(s16x4)>((LDS_PTR(unsigned char))(unsigned long long)((rd.cols ^ (dt << 6) ^ 16) + at + 8 * ROWB)));
         const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
         const u32x4 a = {l2.x, l2.y, h2.x, h2.y};
         acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, p.w[s]), acc[dt],
                                                           0, 0, 0);
       }
   } else {
-    const int h = (threadIdx.x >> 5) & 1;
+    const int h = (threadIdx.x >> 5) & 1, c = (threadIdx.x & 31) >> 2;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int base = (r / 4) * 8 + r % 4;      // this lane reads row base + 4 h
       const unsigned z = (unsigned)(swz<T, D>(base) ^ (h << 3));       // swz(base + 4 h): bit 2 of the row is bit 3 of the swizzle
 #pragma unroll
       for (int dt = 0; dt < Geo<T, D>::NDT; ++dt) {
-        const float a = lds_read<float>(rd.cols[0] + off + (ROW0 + base) * ROWB + (((8 * dt + rd.cols[1]) ^ z) << 4));
+        const float a = lds_read<float>(rd.cols + off + (ROW0 + base) * ROWB + (((8 * dt + c) ^ z) << 4));
         acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.w[r], acc[dt], 0, 0, 0);
       }
     }
@@ -216,7 +236,37 @@ __device__ inline float max_of(const f32x16& s) {
   return t;
 }
 
-// tanh.  bf16 paths: from one exponential and one reciprocal, absolute error about 1e-7.
+// s = mult tanh(to_cap s), to_cap > 0, for 32 rows' worth of scores.  bf16: capped scores mostly stay far below the cap, where a
+// polynomial (odd, degree 7, fitted here to a relative 1e-7 for |x| <= 0.4) takes six plain operations; a wave with a score
+// beyond takes one exponential and one reciprocal for those, a quarter of the rate each (16 heads of 16 384, forward, 1 345 us
+// with those alone).  Absolute error 1e-7 mult either way.
+template <typename T> __device__ inline void cap_scores(f32x16& s, float to_cap, float mult) {
+  if (sizeof(T) == 4) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = mult * tanhf(s[r] * to_cap);
+    return;
+  }
+  float top = fabsf(s[0]);
+#pragma unroll
+  for (int r = 1; r < 16; r += 3) top = fmaxf(fmaxf(fabsf(s[r]), fabsf(s[r + 1])), fmaxf(fabsf(s[r + 2]), top));
+  const float c0 = mult * 9.999999019e-01f, c1 = mult * -3.333136246e-01f, c2 = mult * 1.327097675e-01f, c3 = mult * -4.755360305e-02f;
+  auto near = [&](float x) INLINE {
+    const float u = x * x;
+    return x * fmaf(fmaf(fmaf(c3, u, c2), u, c1), u, c0);
+  };
+  if (__builtin_expect(__any(!(top * to_cap <= 0.4f)), 0)) {
+    // score by score, so that what a row gives does not hang on its neighbours
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float x = s[r] * to_cap;
+      const float far = fmaf(-2.f * mult, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f), mult);
+      s[r] = fabsf(x) <= 0.4f ? near(x) : far;
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = near(s[r] * to_cap);
+  }
+}
 template <typename T> __device__ inline float tanh_of(float x) {
   if (sizeof(T) == 4) return tanhf(x);
   return fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f), 1.f);
@@ -254,6 +304,21 @@ template <typename T, int D> __device__ inline void clean_tile(LDS_PTR(unsigned 
       const int r = at / G::ROWB;
       atomicOr((unsigned*)(bad + (r >> 5)), 1u << (r & 31));
     }
+  }
+}
+
+// A walk over double-buffered tiles, trip(i, parity).  In bf16 two at a time, so that the stages lie at offsets known when
+// compiled, which every read from LDS then has in its instruction (24 heads of 4 608, forward 290 -> 272 us, backward 1 280 ->
+// 1 212).  In fp32, which waits for its products, the copy only costs registers (8 heads of 4 500, causal, 561 -> 994).
+template <typename T, typename Trip> __device__ inline void walk_stages(int begin, int end, const Trip& trip) {
+  if constexpr (sizeof(T) == 2) {
+    for (int i = begin; i < end; i += 2) {
+      trip(i, std::integral_constant<int, 0>{});
+      if (i + 1 >= end) break;
+      trip(i + 1, std::integral_constant<int, 1>{});
+    }
+  } else {
+    for (int i = begin; i < end; ++i) trip(i, (i - begin) & 1);
   }
 }
 
