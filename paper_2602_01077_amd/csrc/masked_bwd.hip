@@ -30,36 +30,32 @@ struct Plan {
 };
 
 // Nothing is moved across, where registers are short.
-template <bool TIGHT> __device__ inline void phase() {
+template <bool TIGHT> __device__ __forceinline__ void phase() {
   if (TIGHT) __builtin_amdgcn_sched_barrier(0);
 }
 
 // A score and what its gradient is multiplied by.
 template <typename T, int MOD> struct Scorer {
-  float c, to_cap, cap, slope;
-  __device__ inline Scorer(const Masked& p, int head) {
+  float c, to_cap, slope;
+  __device__ __forceinline__ Scorer(const Masked& p, int head) {
     const float u = sizeof(T) == 2 ? kLog2e : 1.f;
-    c = MOD ? 1.f : p.scale * u;
-    to_cap = MOD & CAP ? p.scale / p.cap : p.scale * u;
-    cap = p.cap * u;
+    c = (MOD & CAP ? p.cap : p.scale) * u;
+    to_cap = MOD & CAP ? p.scale / p.cap : 0.f;
     slope = MOD & BIAS ? p.slopes[head] * u : 0.f;
   }
   // raw products to what weight() takes: capped ones to their tanh
-  __device__ inline void prepare(f32x16& s) const {
+  __device__ __forceinline__ void prepare(f32x16& s) const {
     if (MOD & CAP) cap_scores<T>(s, to_cap, 1.f);
   }
-  // the weight exp(z - lse); `far` = |pos - key|; *gain = dz/ds
-  __device__ inline float weight(float s, float minus_lse, float far, float* gain) const {
-    *gain = 1.f;
-    if (!MOD) return exp_diff<T>(s, c, minus_lse);
-    if (MOD & CAP) *gain = (1.f - s) * (1.f + s);
-    const float z = s * (MOD & CAP ? cap : to_cap);
-    return exp_diff<T>(MOD & BIAS ? fmaf(-slope, far, z) : z, 1.f, minus_lse);
+  // the weight exp(z - lse); `far` = pos - key; *gain = dz/ds
+  __device__ __forceinline__ float weight(float s, float minus_lse, float far, float* gain) const {
+    *gain = MOD & CAP ? (1.f - s) * (1.f + s) : 1.f;
+    return exp_diff<T>(s, c, MOD & BIAS ? fmaf(-slope, fabsf(far), minus_lse) : minus_lse);
   }
 };
-template <typename T> __device__ inline float in_domain(float lse) { return sizeof(T) == 2 ? lse * kLog2e : lse; }
+template <typename T> __device__ __forceinline__ float in_domain(float lse) { return sizeof(T) == 2 ? lse * kLog2e : lse; }
 
-__device__ inline Span span_of_group(const Span& ws, int (*span_s)[4], int wave, int lane) {
+__device__ __forceinline__ Span span_of_group(const Span& ws, int (*span_s)[4], int wave, int lane) {
   if (lane == 0) {
     span_s[wave][0] = ws.lo;
     span_s[wave][1] = ws.hi;
@@ -74,7 +70,7 @@ __device__ inline Span span_of_group(const Span& ws, int (*span_s)[4], int wave,
               __builtin_amdgcn_readfirstlane(gs.full_hi)};
 }
 
-template <typename T> __device__ inline float dot16(u32x4 a, u32x4 b) {      // of 16 bytes each
+template <typename T> __device__ __forceinline__ float dot16(u32x4 a, u32x4 b) {      // of 16 bytes each
   float d = 0.f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -90,7 +86,7 @@ template <typename T> __device__ inline float dot16(u32x4 a, u32x4 b) {      // 
 
 // The lane's row of sums, times f; zeros unless `some` (the sums of a row that has none can hold anything).
 template <typename T, int D>
-__device__ inline void store_row(unsigned char* dst, const f32x16 (&acc)[Geo<T, D>::NDT], float f, bool some, int h) {
+__device__ __forceinline__ void store_row(unsigned char* dst, const f32x16 (&acc)[Geo<T, D>::NDT], float f, bool some, int h) {
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
@@ -216,6 +212,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
       Weights<T> w;
       const unsigned n = (unsigned)(iv.hi - iv.lo);
       const int key0 = t * kRows + ROW0 + 4 * h;
+      const float ahead = (float)(pos - key0);
       float top = 0.f;
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
@@ -224,7 +221,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
         for (int u = 0; u < 2; ++u) {
           const int key = key0 + ((r + u) / 4) * 8 + (r + u) % 4;
           float gain;
-          float wt = sc.weight(s[r + u], minus_lse, fabsf((float)(pos - key)), &gain);
+          float wt = sc.weight(s[r + u], minus_lse, ahead - (float)(((r + u) / 4) * 8 + (r + u) % 4), &gain);
           x[u] = wt * (dp[r + u] - delta);
           if (part && (unsigned)(key - lo) >= n) wt = x[u] = 0.f;
           if (MENDS) {
@@ -240,7 +237,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
         for (int r = 0; r < 16; ++r) {
           const int key = key0 + (r / 4) * 8 + r % 4;
           float gain;
-          const float wt = sc.weight(s[r], minus_lse, fabsf((float)(pos - key)), &gain);
+          const float wt = sc.weight(s[r], minus_lse, ahead - (float)((r / 4) * 8 + r % 4), &gain);
           if (wt >= kHeavy && (unsigned)(key - lo) < n && n_heavy < kMostHeavy) {
             heavy[n_heavy][tid].key = key;
             heavy[n_heavy][tid].weight = wt * gain;
@@ -415,7 +412,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel
         lo = seen_s[own].lo;
         count = (unsigned)(seen_s[own].hi - lo);
       }
-      const int row0 = x0 + ROW0 + 4 * h, key = kt * kOwn + own;
+      const int row0 = x0 + ROW0 + 4 * h;
+      const float ahead = (float)(row0 + shift - (kt * kOwn + own));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const f32x4 ml = *reinterpret_cast<LDS_PTR(const f32x4)>((LDS_PTR(const float))&stat[par][0][ROW0 + 8 * e + 4 * h]);
@@ -425,7 +423,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel
         for (int u = 0; u < 4; ++u) {
           const int r = 4 * e + u, row = row0 + 8 * e + u;
           float gain;
-          x[u] = sc.weight(s[r], ml[u], fabsf((float)(row + shift - key)), &gain);
+          x[u] = sc.weight(s[r], ml[u], ahead + (float)(8 * e + u), &gain);
           y[u] = x[u] * (dp[r] - de[u]);
           if (MOD & CAP) y[u] *= gain;
           if (part) {

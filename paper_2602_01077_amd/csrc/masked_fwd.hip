@@ -32,7 +32,7 @@ template <typename T, int D> struct Row {        // what a lane holds of its que
 };
 
 // The maximum takes in t (this lane's largest score); l and o are rescaled if some lane's moved.
-template <typename T, int D> __device__ inline void raise_max(Row<T, D>& st, float t) {
+template <typename T, int D> __device__ __forceinline__ void raise_max(Row<T, D>& st, float t) {
   t = fmaxf(t, __shfl_xor(t, 32));
   const float m = fmaxf(st.m, t);
   if (__any(m != st.m)) {
@@ -44,15 +44,48 @@ template <typename T, int D> __device__ inline void raise_max(Row<T, D>& st, flo
   }
 }
 
-// Weights of 32 keys against the maximum as it stands, and their sum.
-template <typename T> __device__ inline float weigh(const f32x16& s, float c, float minus_m, Weights<T>& w) {
+// What a wave's scores are made of: raw products times c, or their capped form, less slope times the distance.  The log2 domain
+// in bf16.
+template <typename T, int MOD> struct Score {
+  float c, to_cap, cap, slope, near_limit;
+  bool direct;
+  Near near;             // in raw products, if direct
+  __device__ __forceinline__ Score(const Masked& p, int head) : near(0.f) {
+    const float unit = sizeof(T) == 2 ? kLog2e : 1.f;
+    c = MOD & CAP ? 1.f : p.scale * unit;
+    to_cap = MOD & CAP ? p.scale / p.cap : 0.f;
+    cap = p.cap * unit;
+    slope = MOD & BIAS ? p.slopes[head] * unit : 0.f;
+    direct = (MOD & CAP) && Near::all_direct(cap, to_cap);
+    near_limit = MOD & CAP ? (kNear / to_cap) * (kNear / to_cap) : 0.f;
+    if (direct) {
+      near = Near(cap);
+      near.rescale(to_cap);
+    }
+  }
+};
+
+// Weights of 32 keys against the maximum as it stands, and their sum.  ahead: the row's position, counted from this lane's
+// first key.  NEAR: s holds raw products, taken to be below the cap: the last step of their polynomial takes off the maximum,
+// and their largest square, by which the caller sees whether they were, goes to top.
+template <typename T, int MOD, bool NEAR>
+__device__ __forceinline__ float weigh(const Score<T, MOD>& sc, const f32x16& s, float c, float slope, float minus_m, float ahead,
+                                       Weights<T>& w, float& top) {
   float a = 0.f, b = 0.f;
 #pragma unroll
   for (int r = 0; r < 16; r += 2) {
-    const float x = exp_diff<T>(s[r], c, minus_m), y = exp_diff<T>(s[r + 1], c, minus_m);
-    w.set(r, x, y);
-    if (r & 2) b += x + y;
-    else a += x + y;
+    float x[2], u[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int key = ((r + e) / 4) * 8 + (r + e) % 4;
+      const float m = MOD & BIAS ? fmaf(-slope, fabsf(ahead - (float)key), minus_m) : minus_m;
+      u[e] = s[r + e] * s[r + e];
+      x[e] = exp_diff<T>(s[r + e], NEAR ? sc.near.of(u[e]) : c, m);
+    }
+    if (NEAR) top = fmaxf(fmaxf(u[0], u[1]), top);
+    w.set(r, x[0], x[1]);
+    if (r & 2) b += x[0] + x[1];
+    else a += x[0] + x[1];
   }
   return a + b;
 }
@@ -111,11 +144,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
       if (sees) q[s] = *reinterpret_cast<const u32x4*>(src + 32 * s + 16 * h);
     }
   }
-  // Scores: raw products times c, or, capped or biased, made final in place and c = 1.  The log2 domain in bf16.
-  const float unit_scale = sizeof(T) == 2 ? kLog2e : 1.f;
-  const float c = MOD ? 1.f : p.scale * unit_scale;
-  const float to_cap = MOD & CAP ? p.scale / p.cap : p.scale * unit_scale, cap = p.cap * unit_scale;
-  const float slope = MOD & BIAS ? p.slopes[head] * unit_scale : 0.f;
+  const Score<T, MOD> sc(p, head);
   const int pos = row + p.kv_len - p.q_len;
 
   Row<T, D> st;
@@ -141,6 +170,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
     t_end = first + (int)((long long)n * (share.part + 1) / plan.deal.n_parts);
   }
 
+  // The walk: ascending; where scores fall with the distance, from the rows' own tile down and then up from it, so that the
+  // running maximum is met at once (a rising one is taken anew all the time: 24 / 8 heads of 500 rows, 9 001 keys, 110 us).
+  const int n_tiles = t_end - t_begin;
+  int start = t_begin, down = 0;
+  if ((MOD & BIAS) && n_tiles > 0) {
+    start = min(max((min(qt * kQRows + kQRows, p.q_len) - 1 + p.kv_len - p.q_len) / kRows, t_begin), t_end - 1);
+    down = start - t_begin + 1;
+  }
+  auto tile_at = [&](int i) INLINE { return !(MOD & BIAS) ? t_begin + i : i < down ? start - i : t_begin + i; };
+
   auto load_k = [&](int t, int stage_at) INLINE {
     lk.load(wave, lane, kg + (long long)t * kRows * p.sk.token, p.kv_len - t * kRows, lds + stage_at * TILEB);
   };
@@ -152,40 +191,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
     if (!touches(ws, t * kRows, kRows)) return;
     s0 = rows_times<T, D, 0>(rd, off, q);
     s1 = rows_times<T, D, 32>(rd, off, q);
-    if (MOD & CAP) {
-      cap_scores<T>(s0, to_cap, cap);
-      cap_scores<T>(s1, to_cap, cap);
-    }
-    if (MOD & BIAS) {
-      const int ahead = pos - t * kRows - 4 * h;   // of key 0 of this lane's
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int key = (r / 4) * 8 + r % 4;
-        if (!(MOD & CAP)) {
-          s0[r] *= to_cap;
-          s1[r] *= to_cap;
-        }
-        s0[r] = fmaf(-slope, fabsf((float)(ahead - key)), s0[r]);
-        s1[r] = fmaf(-slope, fabsf((float)(ahead - key - 32)), s1[r]);
-      }
-    }
   };
 
-  if (t_begin < t_end) {
-    load_k(t_begin, 0);
+  if (n_tiles > 0) {
+    load_k(tile_at(0), 0);
     wait_loads();
     __syncthreads();
-    if (t_begin + 1 < t_end) load_k(t_begin + 1, 1);
-    load_v(t_begin, 0);
-    scores(t_begin, 0);
+    if (n_tiles > 1) load_k(tile_at(1), 1);
+    load_v(tile_at(0), 0);
+    scores(tile_at(0), 0);
   }
-  auto trip = [&](int t, auto parity) INLINE {
-    const int par = parity;
+  auto trip = [&](int i, auto parity) INLINE {
+    const int par = parity, t = tile_at(i);
     const unsigned v_off = (2 + par) * TILEB;
     wait_loads();
     __syncthreads();
-    if (t + 2 < t_end) load_k(t + 2, par);
-    if (t + 1 < t_end) load_v(t + 1, par ^ 1);
+    if (i + 2 < n_tiles) load_k(tile_at(i + 2), par);
+    if (i + 1 < n_tiles) load_v(tile_at(i + 1), par ^ 1);
     unsigned bad0 = 0u, bad1 = 0u;
     if (!covers(gs, t * kRows, kRows)) {         // seen in part by some row of the workgroup
       clean_tile<T, D>((LDS_PTR(unsigned char))&stage[0] + v_off, (LDS_PTR(unsigned))&bad[0], tid);
@@ -198,35 +220,62 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
       }
     }
     if (touches(ws, t * kRows, kRows)) {
-      if (!covers(ws, t * kRows, kRows)) {
-        const unsigned n = (unsigned)(iv.hi - iv.lo);
-        const int at = t * kRows + 4 * h - iv.lo;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = (r / 4) * 8 + r % 4;
-          if ((unsigned)(at + key) >= n) s0[r] = -INFINITY;
-          if ((unsigned)(at + key + 32) >= n) s1[r] = -INFINITY;
-        }
-      }
+      const float ahead = MOD & BIAS ? (float)(pos - t * kRows - 4 * h) : 0.f;
+      const bool whole = covers(ws, t * kRows, kRows);
+      bool near = sizeof(T) == 2 && (MOD & CAP) && whole && sc.direct;
       Weights<T> w0, w1;
-      float sum = weigh<T>(s0, c, -st.m, w0) + weigh<T>(s1, c, -st.m, w1);
+      float sum, top = 0.f;
+      if (near) {
+        sum = weigh<T, MOD, true>(sc, s0, 1.f, sc.slope, -st.m, ahead, w0, top);
+        sum += weigh<T, MOD, true>(sc, s1, 1.f, sc.slope, -st.m, ahead - 32.f, w1, top);
+        near = !__any(!(top <= sc.near_limit));
+      }
+      if (!near) {
+        if (MOD & CAP) {
+          cap_scores<T>(s0, sc.to_cap, sc.cap);
+          cap_scores<T>(s1, sc.to_cap, sc.cap);
+        }
+        if (!whole) {
+          const unsigned n = (unsigned)(iv.hi - iv.lo);
+          const int at = t * kRows + 4 * h - iv.lo;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int key = (r / 4) * 8 + r % 4;
+            if ((unsigned)(at + key) >= n) s0[r] = -INFINITY;
+            if ((unsigned)(at + key + 32) >= n) s1[r] = -INFINITY;
+          }
+        }
+        sum = weigh<T, MOD, false>(sc, s0, sc.c, sc.slope, -st.m, ahead, w0, top);
+        sum += weigh<T, MOD, false>(sc, s1, sc.c, sc.slope, -st.m, ahead - 32.f, w1, top);
+      }
       if (__builtin_expect(__any(!(sum < kStaleLimit)), 0)) {
-        // Row by row, so that what a row gives does not hang on its neighbours.  The products are rounded as the maximum is
-        // taken of them: the largest key has weight 1, whatever its size.
+        // Row by row, so that what a row gives does not hang on its neighbours.  The scores are rounded as the maximum is taken
+        // of them: the largest key has weight 1, whatever its size.
         bool again = !(sum < kStaleLimit);
         again |= (bool)__shfl_xor((int)again, 32);
-        const float f = again ? c : 1.f, c2 = again ? 1.f : c;
+        if (near) {
+          cap_scores<T>(s0, sc.to_cap, sc.cap);
+          cap_scores<T>(s1, sc.to_cap, sc.cap);
+        }
+        const float f = again ? sc.c : 1.f, c2 = again ? 1.f : sc.c;
+        const float slope1 = again ? sc.slope : 0.f, slope2 = again ? 0.f : sc.slope;
         {
 #pragma clang fp contract(off)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
+            const float key = (float)((r / 4) * 8 + r % 4);
             s0[r] *= f;
             s1[r] *= f;
+            if (MOD & BIAS) {
+              s0[r] -= slope1 * fabsf(ahead - key);
+              s1[r] -= slope1 * fabsf(ahead - 32.f - key);
+            }
           }
         }
         raise_max<T, D>(st, again ? fmaxf(max_of(s0), max_of(s1)) : -INFINITY);
         const float nm = st.m == -INFINITY ? 0.f : -st.m;
-        sum = weigh<T>(s0, c2, nm, w0) + weigh<T>(s1, c2, nm, w1);
+        sum = weigh<T, MOD, false>(sc, s0, c2, slope2, nm, ahead, w0, top);
+        sum += weigh<T, MOD, false>(sc, s1, c2, slope2, nm, ahead - 32.f, w1, top);
       }
       st.l += sum;
       cols_times<T, D, 0>(rd, v_off, w0, st.o);
@@ -248,9 +297,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel
           }
       }
     }
-    if (t + 1 < t_end) scores(t + 1, (par ^ 1) * TILEB);
+    if (i + 1 < n_tiles) scores(tile_at(i + 1), (par ^ 1) * TILEB);
   };
-  walk_stages<T>(t_begin, t_end, trip);
+  walk_stages<T>(0, n_tiles, trip);
 
   st.l += __shfl_xor(st.l, 32);
   if (plan.deal.n_parts > 1) {

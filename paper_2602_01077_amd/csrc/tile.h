@@ -27,7 +27,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// for lambdas that hold a wave's registers by reference: called out of line, those would lie in memory
+// Lambdas and functions that take a wave's registers by reference: called out of line, those would lie in memory.
 #define INLINE __attribute__((always_inline))
 #define LDS_PTR(T) __attribute__((address_space(3))) T*
 
@@ -35,7 +35,7 @@ constexpr int kRows = 64;                        // rows of a staged tile
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // The lane number, made anew where it stands: for loops that have no register to keep it in.
-__device__ inline int lane_anew() {
+__device__ __forceinline__ int lane_anew() {
   int lane;
   asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
   return lane;
@@ -64,14 +64,14 @@ template <typename T, int D> __host__ __device__ constexpr int swz(int r) {
 // LDS-DMA of 1 KB: lane l's 16 bytes go to lds + 16 l.  In inline asm, so that the compiler puts no wait on it in front of
 // reads of another stage; wait_loads() and a barrier come before the tile is read.  A scalar write of M0 needs one wait
 // state before the load reads it.
-__device__ inline void dma_1kb(unsigned lds, unsigned voff, const unsigned char* base /* both uniform */) {
+__device__ __forceinline__ void dma_1kb(unsigned lds, unsigned voff, const unsigned char* base /* both uniform */) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory", "m0");
 }
 // The same for one 4-byte word a lane.
-__device__ inline void dma_words(unsigned lds, unsigned voff, const void* base /* uniform, as lds */) {
+__device__ __forceinline__ void dma_words(unsigned lds, unsigned voff, const void* base /* uniform, as lds */) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(voff), "s"(base) : "memory", "m0");
 }
-__device__ inline void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }     // vmcnt(0), the other counters left alone
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }     // vmcnt(0), the other counters left alone
 
 // A wave's part in loading tiles of a tensor with `stride` bytes from row to row: rows 16 wave .. + 15, piece i of them rows
 // RPL i .. + RPL - 1.  Rows past `avail` (>= 1) are replaced by the last valid one; the caller masks them.
@@ -83,14 +83,14 @@ template <typename T, int D, bool ANEW = false> struct Loader {
   static_assert(G::RPL * G::NLD == 16, "a wave loads 16 rows, the swizzle's period");
   unsigned stride;
   unsigned off[ANEW ? 1 : G::NLD];               // byte offset from the tile's first row, piece by piece
-  __device__ inline static int row(int wave, int lane, int i) { return G::RPL * (G::NLD * wave + i) + lane / G::CPR; }
-  __device__ inline static unsigned chunk(int lane, int r) { return (unsigned)(((lane % G::CPR) ^ swz<T, D>(r)) << 4); }
-  __device__ inline void init(int wave, int lane, unsigned stride_) {
+  __device__ __forceinline__ static int row(int wave, int lane, int i) { return G::RPL * (G::NLD * wave + i) + lane / G::CPR; }
+  __device__ __forceinline__ static unsigned chunk(int lane, int r) { return (unsigned)(((lane % G::CPR) ^ swz<T, D>(r)) << 4); }
+  __device__ __forceinline__ void init(int wave, int lane, unsigned stride_) {
     stride = stride_;
 #pragma unroll
     for (int i = 0; i < (ANEW ? 0 : G::NLD); ++i) off[i] = (unsigned)row(wave, lane, i) * stride + chunk(lane, row(wave, lane, i));
   }
-  __device__ inline void load(int wave, int lane, const unsigned char* base, int avail, unsigned lds) const {
+  __device__ __forceinline__ void load(int wave, int lane, const unsigned char* base, int avail, unsigned lds) const {
     const unsigned at = __builtin_amdgcn_readfirstlane(lds + wave * (G::NLD * 1024));
     if constexpr (ANEW) {
       lane = lane_anew();
@@ -122,7 +122,7 @@ template <typename T, int D> struct Reader {
   using G = Geo<T, D>;
   unsigned rows;                                 // 16 bytes of row lam, contraction step 0
   unsigned cols;                                 // columns: bf16, rows 0..7 of a contraction step of 16 (8..15: bit 4 flips)
-  __device__ inline void init(int lane, unsigned tile) {
+  __device__ __forceinline__ void init(int lane, unsigned tile) {
     const int lam = lane & 31, h = lane >> 5;
     rows = tile + lam * G::ROWB + ((h ^ swz<T, D>(lam)) << 4);
     if (sizeof(T) == 2) {
@@ -136,12 +136,12 @@ template <typename T, int D> struct Reader {
   }
 };
 
-template <typename V> __device__ inline V lds_read(unsigned at) {
+template <typename V> __device__ __forceinline__ V lds_read(unsigned at) {
   return *reinterpret_cast<LDS_PTR(const V)>((LDS_PTR(const unsigned char))(unsigned long long)at);
 }
 
 // One contraction step over channels (32 bytes of each row): acc += A B.
-template <typename T> __device__ inline f32x16 mma_step(u32x4 a, u32x4 b, f32x16 acc) {
+template <typename T> __device__ __forceinline__ f32x16 mma_step(u32x4 a, u32x4 b, f32x16 acc) {
   if constexpr (sizeof(T) == 2) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
   } else {
@@ -154,7 +154,7 @@ template <typename T> __device__ inline f32x16 mma_step(u32x4 a, u32x4 b, f32x16
 
 // acc = (32 rows of the tile, from row ROW0) * (the lane's own row, all channels).  OFF: byte offset of the tile.
 template <typename T, int D, int ROW0>
-__device__ inline f32x16 rows_times(const Reader<T, D>& rd, unsigned off, const u32x4 (&b)[Geo<T, D>::STEPS]) {
+__device__ __forceinline__ f32x16 rows_times(const Reader<T, D>& rd, unsigned off, const u32x4 (&b)[Geo<T, D>::STEPS]) {
   f32x16 acc = (f32x16){0};
 #pragma unroll
   for (int s = 0; s < Geo<T, D>::STEPS; ++s)
@@ -162,7 +162,7 @@ __device__ inline f32x16 rows_times(const Reader<T, D>& rd, unsigned off, const 
   return acc;
 }
 
-__device__ inline unsigned pack_bf16(float lo, float hi) {
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
   f32x2 f = {lo, hi};
   bf16x2 b = __builtin_convertvector(f, bf16x2);
   return __builtin_bit_cast(unsigned, b);
@@ -172,11 +172,11 @@ __device__ inline unsigned pack_bf16(float lo, float hi) {
 template <typename T> struct Weights;
 template <> struct Weights<__bf16> {
   u32x4 w[2];
-  __device__ inline void set(int r, float a, float b) { w[r >> 3][(r & 7) >> 1] = pack_bf16(a, b); }    // rows r, r + 1 (r even)
+  __device__ __forceinline__ void set(int r, float a, float b) { w[r >> 3][(r & 7) >> 1] = pack_bf16(a, b); }    // rows r, r + 1 (r even)
 };
 template <> struct Weights<float> {
   f32x16 w;
-  __device__ inline void set(int r, float a, float b) {
+  __device__ __forceinline__ void set(int r, float a, float b) {
     w[r] = a;
     w[r + 1] = b;
   }
@@ -184,7 +184,7 @@ template <> struct Weights<float> {
 
 // acc[dt] += (32 rows of the tile, from row ROW0)^T (channels x rows) * weights (rows x the lane's column).
 template <typename T, int D, int ROW0>
-__device__ inline void cols_times(const Reader<T, D>& rd, unsigned off, const Weights<T>& p, f32x16 (&acc)[Geo<T, D>::NDT]) {
+__device__ __forceinline__ void cols_times(const Reader<T, D>& rd, unsigned off, const Weights<T>& p, f32x16 (&acc)[Geo<T, D>::NDT]) {
   constexpr int ROWB = Geo<T, D>::ROWB;
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -219,55 +219,71 @@ __device__ inline void cols_times(const Reader<T, D>& rd, unsigned off, const We
 // exp of a difference of scores.  Scores are kept in the log2 domain in bf16 (the exponent is one fused operation) and in the
 // natural one in fp32, where the rounded constant would cost the last digits: z - m is one fused operation on the raw
 // product, small where the weight is not, and only then multiplied.
-template <typename T> __device__ inline float exp_diff(float s, float c, float minus_m) {
+template <typename T> __device__ __forceinline__ float exp_diff(float s, float c, float minus_m) {
   if (sizeof(T) == 2) return __builtin_amdgcn_exp2f(fmaf(s, c, minus_m));
   return __builtin_amdgcn_exp2f(fmaf(s, c, minus_m) * kLog2e);
 }
-template <typename T> __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(sizeof(T) == 2 ? x : x * kLog2e); }
+template <typename T> __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(sizeof(T) == 2 ? x : x * kLog2e); }
 // log of a sum of weights in that domain, and its way to the natural one
-template <typename T> __device__ inline float log_sum(float m, float l) {
+template <typename T> __device__ __forceinline__ float log_sum(float m, float l) {
   return sizeof(T) == 2 ? (m + __builtin_amdgcn_logf(l)) * kLn2 : m + logf(l);
 }
 
-__device__ inline float max_of(const f32x16& s) {
+__device__ __forceinline__ float max_of(const f32x16& s) {
   float t = s[0];
 #pragma unroll
   for (int r = 1; r < 16; ++r) t = fmaxf(t, s[r]);
   return t;
 }
 
-// s = mult tanh(to_cap s), to_cap > 0, for 32 rows' worth of scores.  bf16: capped scores mostly stay far below the cap, where a
-// polynomial (odd, degree 7, fitted here to a relative 1e-7 for |x| <= 0.4) takes six plain operations; a wave with a score
-// beyond takes one exponential and one reciprocal for those, a quarter of the rate each (16 heads of 16 384, forward, 1 345 us
-// with those alone).  Absolute error 1e-7 mult either way.
-template <typename T> __device__ inline void cap_scores(f32x16& s, float to_cap, float mult) {
+// tanh of capped scores.  bf16: they mostly stay far below the cap, where an odd polynomial of degree 7 (fitted here to a
+// relative 1e-7 for |x| <= 0.4) takes six plain operations; beyond, one exponential and one reciprocal, a quarter of the rate
+// each, absolute error 1e-7.
+constexpr float kNear = 0.4f;
+struct Near {                                    // mult tanh(x) = x of(x^2)
+  float c0, c1, c2, c3;
+  // the same in s = x / to_cap, mult tanh(to_cap s) = s of(s^2), where no power of it leaves the range of fp32 (all_direct)
+  __device__ __forceinline__ void rescale(float to_cap) {
+    const float u = to_cap * to_cap;
+    c0 *= to_cap;
+    c1 *= to_cap * u;
+    c2 *= to_cap * u * u;
+    c3 *= to_cap * u * u * u;
+  }
+  __device__ __forceinline__ static bool all_direct(float mult, float to_cap) {
+    return to_cap >= 0x1p-16f && to_cap <= 16.f && mult >= 0x1p-8f && mult <= 0x1p20f;
+  }
+  __device__ __forceinline__ Near(float mult) : c0(mult * 9.999999019e-01f), c1(mult * -3.333136246e-01f), c2(mult * 1.327097675e-01f), c3(mult * -4.755360305e-02f) {}
+  __device__ __forceinline__ float of(float u) const { return fmaf(fmaf(fmaf(c3, u, c2), u, c1), u, c0); }
+};
+// s = mult tanh(to_cap s), to_cap > 0, for 32 rows' worth of scores.
+template <typename T> __device__ __forceinline__ void cap_scores(f32x16& s, float to_cap, float mult) {
   if (sizeof(T) == 4) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = mult * tanhf(s[r] * to_cap);
     return;
   }
-  float top = fabsf(s[0]);
+  const Near near(mult);
+  float top = 0.f;
 #pragma unroll
-  for (int r = 1; r < 16; r += 3) top = fmaxf(fmaxf(fabsf(s[r]), fabsf(s[r + 1])), fmaxf(fabsf(s[r + 2]), top));
-  const float c0 = mult * 9.999999019e-01f, c1 = mult * -3.333136246e-01f, c2 = mult * 1.327097675e-01f, c3 = mult * -4.755360305e-02f;
-  auto near = [&](float x) INLINE {
-    const float u = x * x;
-    return x * fmaf(fmaf(fmaf(c3, u, c2), u, c1), u, c0);
-  };
-  if (__builtin_expect(__any(!(top * to_cap <= 0.4f)), 0)) {
-    // score by score, so that what a row gives does not hang on its neighbours
+  for (int r = 0; r < 16; r += 2) {
+    s[r] *= to_cap;
+    s[r + 1] *= to_cap;
+    top = fmaxf(fmaxf(s[r] * s[r], s[r + 1] * s[r + 1]), top);
+  }
+  if (__builtin_expect(!__any(!(top <= kNear * kNear)), 1)) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] *= near.of(s[r] * s[r]);
+  } else {                                       // score by score, so that what a row gives does not hang on its neighbours
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const float x = s[r] * to_cap;
+      const float x = s[r];
       const float far = fmaf(-2.f * mult, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f), mult);
-      s[r] = fabsf(x) <= 0.4f ? near(x) : far;
+      s[r] = fabsf(x) <= kNear ? x * near.of(x * x) : far;
     }
-  } else {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = near(s[r] * to_cap);
   }
 }
-template <typename T> __device__ inline float tanh_of(float x) {
+template <typename T> __device__ __forceinline__ float tanh_of(float x) {
   if (sizeof(T) == 4) return tanhf(x);
   return fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f), 1.f);
 }
@@ -275,7 +291,7 @@ template <typename T> __device__ inline float tanh_of(float x) {
 // Non-finite elements of a staged tile are set to 0, and the rows they were in marked in bad[0..1] (64 bits, zero before).  A
 // product contracts over all rows of a tile, also where the weight is 0, and 0 * inf is NaN: tiles that are masked in part are
 // cleaned first.  All 256 threads; a barrier before and after is the caller's.
-template <typename T, int D> __device__ inline void clean_tile(LDS_PTR(unsigned char) stage, LDS_PTR(unsigned) bad, int tid) {
+template <typename T, int D> __device__ __forceinline__ void clean_tile(LDS_PTR(unsigned char) stage, LDS_PTR(unsigned) bad, int tid) {
   using G = Geo<T, D>;
 #pragma unroll
   for (int i = 0; i < G::TILEB / 4096; ++i) {
@@ -310,7 +326,7 @@ template <typename T, int D> __device__ inline void clean_tile(LDS_PTR(unsigned 
 // A walk over double-buffered tiles, trip(i, parity).  In bf16 two at a time, so that the stages lie at offsets known when
 // compiled, which every read from LDS then has in its instruction (24 heads of 4 608, forward 290 -> 272 us, backward 1 280 ->
 // 1 212).  In fp32, which waits for its products, the copy only costs registers (8 heads of 4 500, causal, 561 -> 994).
-template <typename T, typename Trip> __device__ inline void walk_stages(int begin, int end, const Trip& trip) {
+template <typename T, typename Trip> __device__ __forceinline__ void walk_stages(int begin, int end, const Trip& trip) {
   if constexpr (sizeof(T) == 2) {
     for (int i = begin; i < end; i += 2) {
       trip(i, std::integral_constant<int, 0>{});
