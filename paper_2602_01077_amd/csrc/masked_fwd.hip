@@ -384,7 +384,8 @@ int parts_of(const Masked& m) {
   } else if (triangle) {
     // fp32 products take so long that three workgroups a compute unit pay (8 heads of 4 500: one part 850, two 574, three
     // 561, six 586), two at 64 channels.
-    parts = std::min(((m.d == 64 ? 64 : 96) + u - 1) / u, tiles / 2);
+    // Two tiles or more to a part; one where all parts still find a compute unit each (2 heads of 300 40 -> 25).
+    parts = std::max(std::min(((m.d == 64 ? 64 : 96) + u - 1) / u, tiles / 2), std::min(32 / u, tiles));
   } else {
     // whole rounds of the 32 compute units of an XCD, and about a tile's time for a part's own sums and its part in the joining
     long long best = 1LL << 60;

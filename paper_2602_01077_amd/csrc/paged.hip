@@ -23,18 +23,23 @@ constexpr int kCols = 16;                        // query heads of a unit
 
 template <typename T, int D> struct PGeo {
   static constexpr int KT = sizeof(T) == 2 ? 32 : 16;       // keys of a wave and tile
-  static constexpr int TILE = 4 * KT;                       // keys of a tile
   static constexpr int ROWB = D * (int)sizeof(T);
   static constexpr int BYTES = KT * ROWB;                   // staged K (or V) of a wave
   static constexpr int NLD = BYTES / 1024;                  // loads of 1 KB
   static constexpr int CPR = ROWB / 16, RPL = 64 / CPR;
   static constexpr int NDT = D / 16;                        // 16-channel tiles
-  static constexpr int GROUPS = BYTES == 8192 ? 256 : 512;  // workgroups: one or two fit a compute unit's LDS
+  static constexpr int WAVES = 4;
+  static constexpr int THREADS = 64 * WAVES;
+  static constexpr int TILE = WAVES * KT;                   // keys of a tile
+  // workgroups: one or two fit a compute unit's LDS (two of two waves at 8 KB: 171 against 169 us for 48 sequences of up to 8 000)
+  static constexpr int GROUPS = BYTES == 8192 ? 256 : 512;
+  static constexpr int PER = THREADS / kCols;               // threads to a row where the waves' sums are joined
 };
 
 struct PPlan {
   int units;           // of a sequence: key heads x blocks of 16 query heads
   int blocks;          // of 16 query heads to a key head
+  int solo;            // a workgroup to a (sequence, unit), nothing to join
   float* part_o;       // [workgroup][2][16][d] weighted values: of its first unit, of its last
   float* part_ml;      // [workgroup][2][2][16] maximum and sum
   int32_t* owners;     // [seq][unit][2] first and last workgroup; the first's slot is its second if the last has bit 30 set
@@ -81,17 +86,17 @@ template <typename T, int D, int MOD>
 __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(Paged p, PPlan plan) {
   using P = PGeo<T, D>;
   constexpr int KT = P::KT, NKV = 2 * P::NLD;
-  __shared__ __attribute__((aligned(1024))) unsigned char stage[4][2][2][P::BYTES];    // [wave][parity][K, V]
-  __shared__ __attribute__((aligned(16))) int32_t pages[4][2][64];
-  __shared__ long long scratch[4];
-  __shared__ float ml_s[4][2][kCols];
+  __shared__ __attribute__((aligned(1024))) unsigned char stage[P::WAVES][2][2][P::BYTES];    // [wave][parity][K, V]
+  __shared__ __attribute__((aligned(16))) int32_t pages[P::WAVES][2][64];
+  __shared__ long long scratch[P::WAVES];
+  __shared__ float ml_s[P::WAVES][2][kCols];
   __shared__ long long found_s[2];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 15, g = lane >> 4;
 
   // ---- this workgroup's range of tiles, and the sequence it starts in ----
-  // tiles up to and with sequence s0 + tid, from s0; *all: of the 256 sequences
+  // tiles up to and with sequence s0 + tid, from s0; *all: of the next THREADS sequences
   auto scan = [&](int s0, long long* all) {
     const int s = s0 + tid;
     long long incl = s < p.seqs ? (length_of(p, s) + P::TILE - 1) / P::TILE : 0;
@@ -104,19 +109,39 @@ __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(
     if (lane == 63) scratch[wave] = incl;
     __syncthreads();
     for (int w = 0; w < wave; ++w) incl += scratch[w];
-    *all = scratch[0] + scratch[1] + scratch[2] + scratch[3];
+    *all = 0;
+#pragma unroll
+    for (int w = 0; w < P::WAVES; ++w) *all += scratch[w];
     return incl;
   };
-  long long here = 0, incl = scan(0, &here), total = here;
-  for (int s0 = 256; s0 < p.seqs; s0 += 256) {
+  long long x_begin = 0, x_end = 0, total = 0, seq_x = 0;
+  int seq = 0, n_groups = 1;
+  if (plan.solo) {
+    seq = blockIdx.x / plan.units;
+    const int unit = blockIdx.x % plan.units, tiles = (length_of(p, seq) + P::TILE - 1) / P::TILE;
+    x_begin = (long long)unit * tiles;
+    x_end = x_begin + tiles;
+    if (tiles == 0) {
+      const int kv_head = unit / plan.blocks, row = unit % plan.blocks * kCols + tid / P::PER;
+      if (row >= p.group) return;
+      const size_t head = (size_t)seq * p.heads + kv_head * p.group + row;
+      for (int i = tid % P::PER; i < P::CPR; i += P::PER) *reinterpret_cast<u32x4*>(p.out + head * P::ROWB + 16 * i) = u32x4{0, 0, 0, 0};
+      if (p.lse && tid % P::PER == 0) p.lse[head] = -INFINITY;
+      return;
+    }
+  } else {
+  long long here = 0, incl = scan(0, &here);
+  total = here;
+  for (int s0 = P::THREADS; s0 < p.seqs; s0 += P::THREADS) {
     long long more;
     scan(s0, &more);
     total += more;
   }
   total *= plan.units;
-  const int n_groups = (int)min((long long)P::GROUPS, total);
+  n_groups = (int)min((long long)P::GROUPS, total);
   if ((int)blockIdx.x >= n_groups) return;
-  const long long x_begin = first_tile(total, n_groups, blockIdx.x), x_end = first_tile(total, n_groups, blockIdx.x + 1);
+  x_begin = first_tile(total, n_groups, blockIdx.x);
+  x_end = first_tile(total, n_groups, blockIdx.x + 1);
   {
     long long base = 0;                          // tiles of the sequences before s0
     for (int s0 = 0;;) {
@@ -128,14 +153,15 @@ __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(
         found_s[1] = lo;
       }
       base += here;
-      s0 += 256;
+      s0 += P::THREADS;
       if (base * plan.units > x_begin || s0 >= p.seqs) break;      // uniform
       incl = scan(s0, &here);
     }
     __syncthreads();
   }
-  int seq = __builtin_amdgcn_readfirstlane((int)found_s[0]);
-  long long seq_x = found_s[1];
+  seq = __builtin_amdgcn_readfirstlane((int)found_s[0]);
+  seq_x = found_s[1];
+  }
 
   const unsigned lds_stage = (unsigned)(unsigned long long)(LDS_PTR(unsigned char)) & stage[wave][0][0][0];
   const unsigned lds_pages = (unsigned)(unsigned long long)(LDS_PTR(int32_t)) & pages[wave][0][0];
@@ -310,11 +336,14 @@ __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(
     }
     __syncthreads();
     {
-      const int c = tid / 16, ch0 = (tid % 16) * (D / 16), r = block * kCols + c;
-      const float top = fmaxf(fmaxf(ml_s[0][0][c], ml_s[1][0][c]), fmaxf(ml_s[2][0][c], ml_s[3][0][c]));
-      float f[4], sum = 0.f;
+      constexpr int CH = D / P::PER;             // channels of a thread
+      const int c = tid / P::PER, ch0 = (tid % P::PER) * CH, r = block * kCols + c;
+      float top = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < P::WAVES; ++w) top = fmaxf(top, ml_s[w][0][c]);
+      float f[P::WAVES], sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < P::WAVES; ++w) {
         f[w] = ml_s[w][0][c] == -INFINITY ? 0.f : exp_of<T>(ml_s[w][0][c] - top);
         sum += ml_s[w][1][c] * f[w];
       }
@@ -323,10 +352,10 @@ __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(
       const size_t slot = (size_t)blockIdx.x * 2 + (x == x_begin ? 0 : 1);
       const size_t hd = (size_t)seq * p.heads + kv_head * p.group + r;
 #pragma unroll
-      for (int e = 0; e < D / 16; e += 4) {
+      for (int e = 0; e < CH; e += 4) {
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
+        for (int w = 0; w < P::WAVES; ++w)
           acc += *reinterpret_cast<LDS_PTR(const f32x4)>(reinterpret_cast<LDS_PTR(const float)>((LDS_PTR(unsigned char))&stage[w][0][0][0]) +
                                                          c * D + ch0 + e) * f[w];
         acc *= norm;
@@ -339,13 +368,13 @@ __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(
             *reinterpret_cast<f32x4*>(p.out + (hd * D + ch0 + e) * 4) = acc;
         }
       }
-      if (t0 == 0 && tid == 0) {                 // who has this unit, for the launch that joins
+      if (!plan.solo && t0 == 0 && tid == 0) {   // who has this unit, for the launch that joins
         const long long x1 = x + tiles - 1;
         int32_t* own = plan.owners + ((size_t)seq * plan.units + unit) * 2;
         own[0] = (int)blockIdx.x | (x == x_begin ? 0 : kSecondSlot);
         own[1] = (int)(((x1 + 1) * n_groups - 1) / total);       // the last workgroup whose range starts at or before x1
       }
-      if (tid % 16 == 0) {
+      if (tid % P::PER == 0) {
         if (!whole) {
           plan.part_ml[(slot * 2 + 0) * kCols + c] = top;
           plan.part_ml[(slot * 2 + 1) * kCols + c] = sum;
@@ -457,6 +486,9 @@ PPlan plan_of(const Paged& p) {
   PPlan pl{};
   pl.blocks = (p.group + kCols - 1) / kCols;
   pl.units = p.kv_heads * pl.blocks;
+  // A table of two tiles at most: one workgroup walks them in less time than a second launch takes (8 / 2 heads, tables of 256
+  // tokens 10.1 -> 7.8 us, of 512 10.1 -> 11.2).
+  pl.solo = (long long)p.max_pages * p.page_size <= (p.dtype == PISA_BF16 ? 256 : 128);
   return pl;
 }
 int groups_of(const Paged& p) {
@@ -465,7 +497,7 @@ int groups_of(const Paged& p) {
 }
 
 template <typename T, int D> hipError_t launch_td(const Paged& p, const PPlan& pl, hipStream_t stream) {
-  const dim3 grid(PGeo<T, D>::GROUPS), block(256);
+  const dim3 grid(pl.solo ? p.seqs * pl.units : PGeo<T, D>::GROUPS), block(256);
   switch ((p.cap > 0.f ? CAP : 0) | (p.slopes ? BIAS : 0)) {
     case 0: hipLaunchKernelGGL((paged_kernel<T, D, 0>), grid, block, 0, stream, p, pl); break;
     case CAP: hipLaunchKernelGGL((paged_kernel<T, D, CAP>), grid, block, 0, stream, p, pl); break;
@@ -473,7 +505,7 @@ template <typename T, int D> hipError_t launch_td(const Paged& p, const PPlan& p
     default: hipLaunchKernelGGL((paged_kernel<T, D, CAP | BIAS>), grid, block, 0, stream, p, pl); break;
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || pl.solo) return e;
   hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(p.seqs * pl.units), block, 0, stream, p, pl);
   return hipGetLastError();
 }
