@@ -369,6 +369,12 @@ def _masked_plan(q_size, k_size, v_size, out_size, q_stride, k_stride, v_stride,
     return shape, _lib.pisa_masked_attention_workspace_bytes(shape), _lib.pisa_masked_attention_backward_workspace_bytes(shape)
 
 
+@functools.lru_cache(maxsize=1024)
+def _grad_strides(q_size, k_size, dout_stride, dq_stride, dk_stride, dv_stride):
+    return PisaGradStrides(_strides(q_size, dout_stride, "dout"), _strides(q_size, dq_stride, "dq"),
+                           _strides(k_size, dk_stride, "dk"), _strides(k_size, dv_stride, "dv"))
+
+
 def _masked_call(q, k, v, out, causal, doc_offsets, softcap, scale):
     if k.dtype != q.dtype or v.dtype != q.dtype or out.dtype != q.dtype:
         raise TypeError("q, k, v and out must have one dtype")
@@ -419,13 +425,14 @@ def masked_attention_backward(q, k, v, out, lse, dout, causal: bool = False, doc
                               dv: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """pisa_masked_attention_backward: gradients of masked_attention(...) with the same arguments, from its out and lse and
     the gradient dout of out.  Returns (dq, dk, dv)."""
-    dq, dk, dv = (torch.empty_like(x) if g is None else g for x, g in ((q, dq), (k, dk), (v, dv)))
+    dq = torch.empty_like(q) if dq is None else dq
+    dk = torch.empty_like(k) if dk is None else dk
+    dv = torch.empty_like(v) if dv is None else dv
     shape, _, need = _masked_call(q, k, v, out, causal, doc_offsets, softcap, scale)
     for name, t, like in (("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
         if t.shape != like.shape or t.dtype != like.dtype:
             raise ValueError(f"{name} must have shape {tuple(like.shape)} and dtype {like.dtype}")
-    strides = PisaGradStrides(*(_strides(t.shape, t.stride(), name) for name, t in
-                                (("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv))))
+    strides = _grad_strides(q.shape, k.shape, dout.stride(), dq.stride(), dk.stride(), dv.stride())
     _on_current_device(q, k, v, out, lse, dout, doc_offsets, prefix, slopes, dq, dk, dv)
     keep, ws, size = _workspace(workspace, need, q.device)
     _check(_lib.pisa_masked_attention_backward(
