@@ -259,6 +259,7 @@ int32_t dense_attention(const pisa_shape* shape, const void* q, const void* k, c
  * and no negative number, a token stride below 2^31 / 64 bytes.  Batch or head strides of 0 are allowed for inputs
  * (one tensor for all), not for outputs of more than one batch element or head.  All strides 0: dense
  * [batch, heads, len, head_dim].
+ * batch * heads <= 65535, q_len and kv_len <= 2^24, and 128-row tiles of all heads together below 2^24 - 8.
  * doc_offsets and prefix are read on the device.  Offsets that do not ascend give rows other keys, but no access outside
  * the tensors.
  */
@@ -277,7 +278,7 @@ typedef struct pisa_masked_shape {
   int32_t causal;      /* 0 or 1 */
   int32_t num_docs;    /* >= 0; 0: doc_offsets is NULL */
   float   scale;       /* <= 0 selects 1/sqrt(head_dim) */
-  float   softcap;     /* >= 0; 0: scores are not capped */
+  float   softcap;     /* 0: scores are not capped; else 2^-64 .. 2^64, with scale / softcap within 2^-96 .. 2^96 */
   pisa_strides q, k, v, out;
 } pisa_masked_shape;
 
@@ -326,7 +327,7 @@ int32_t pisa_masked_attention_backward(const pisa_masked_shape* shape, const pis
  * Page numbers outside [0, num_pages) are never followed: what belongs to them is not written, and not attended to.
  */
 typedef struct pisa_paged_shape {
-  int32_t seqs;        /* >= 1 */
+  int32_t seqs;        /* >= 1; seqs * heads < 2^24 */
   int32_t heads;       /* query heads, a multiple of kv_heads */
   int32_t kv_heads;    /* >= 1 */
   int32_t head_dim;    /* 64 or 128 */
@@ -335,7 +336,7 @@ typedef struct pisa_paged_shape {
   int32_t num_pages;   /* >= 1 */
   int32_t max_pages;   /* >= 1: entries in a row of page_table; max_pages * page_size <= 2^30 */
   float   scale;       /* <= 0 selects 1/sqrt(head_dim) */
-  float   softcap;     /* >= 0; 0: none */
+  float   softcap;     /* as above */
   pisa_strides k_pages, v_pages;   /* all 0: dense [num_pages, page_size, kv_heads, d] */
 } pisa_paged_shape;
 
@@ -344,7 +345,7 @@ typedef struct pisa_paged_shape {
  * positions lengths[s] - (offsets[s+1] - offsets[s]) .. lengths[s] - 1; lengths already count them.  Rows outside
  * [offsets[0], offsets[seqs]) and positions below 0 or past the table are not written anywhere.  Nothing else in the cache
  * is touched.  Two rows for one slot (sequences that share a page) leave either.
- *   k, v       [tokens, kv_heads, d], shape->dtype, dense;  tokens >= 0
+ *   k, v       [tokens, kv_heads, d], shape->dtype, dense;  tokens >= 0, tokens * kv_heads * d < 2^32
  *   offsets    int32 [seqs + 1], ascending, on the device
  *   page_table int32 [seqs, max_pages], lengths int32 [seqs], on the device
  */

@@ -38,6 +38,7 @@ int32_t resolve_strides(const char* name, const pisa_strides& s, const Extent& n
     long long stride, n;
   } dims[3] = {{t.batch, n.batch}, {t.head, n.heads}, {t.token, n.len}};
   for (const Dim& x : dims) {
+    if (x.stride > 0 && x.n > (1LL << 56) / x.stride) return fail(PISA_UNSUPPORTED, "%s: stride of %lld elements", name, x.stride);
     if (x.stride < 0) return fail(PISA_INVALID_ARG, "%s: strides must not be negative", name);
     if (x.stride >= (1LL << 40)) return fail(PISA_UNSUPPORTED, "%s: stride of %lld elements", name, x.stride);
     if (x.stride * size % 16 != 0)
@@ -63,6 +64,9 @@ int32_t check_scores(float scale, float softcap, int head_dim, float* resolved) 
   if (!(scale == scale) || std::isinf(scale)) return fail(PISA_INVALID_ARG, "scale is not finite");
   if (!(softcap >= 0.f) || std::isinf(softcap)) return fail(PISA_INVALID_ARG, "softcap must be finite and >= 0");
   *resolved = scale > 0.f ? scale : 1.0f / std::sqrt((float)head_dim);
+  // scores are divided by the cap before it is known how small they are: neither factor may leave the normal range
+  if (softcap > 0.f && !(softcap >= 0x1p-64f && softcap <= 0x1p64f && *resolved / softcap >= 0x1p-96f && *resolved / softcap <= 0x1p96f))
+    return fail(PISA_UNSUPPORTED, "softcap must be 0 or within 2^-64 .. 2^64, and scale / softcap within 2^-96 .. 2^96");
   return PISA_OK;
 }
 int32_t check_type(int dtype, int head_dim) {
@@ -94,7 +98,8 @@ int32_t resolve_masked(const pisa_masked_shape* s, Masked* m) {
   if ((long long)s->batch * s->heads > 65535)
     return fail(PISA_UNSUPPORTED, "batch * heads = %lld exceeds 65535", (long long)s->batch * s->heads);
   const long long tiles = std::max(((long long)s->q_len + 127) / 128, ((long long)s->kv_len + 127) / 128);
-  if ((long long)s->batch * s->heads * tiles >= (1LL << 28)) return fail(PISA_UNSUPPORTED, "tensor too large");
+  // a launch has below 2^32 threads
+  if ((long long)s->batch * s->heads * tiles >= (1LL << 24) - 8) return fail(PISA_UNSUPPORTED, "tensor too large");
   m->batch = s->batch;
   m->heads = s->heads;
   m->kv_heads = s->kv_heads;
@@ -133,8 +138,8 @@ int32_t resolve_paged(const pisa_paged_shape* s, Paged* p) {
   if (rc != PISA_OK) return rc;
   if ((long long)s->max_pages * s->page_size > (1LL << 30))
     return fail(PISA_UNSUPPORTED, "a row of the page table may hold at most 2^30 tokens (got %lld)", (long long)s->max_pages * s->page_size);
-  if ((long long)s->seqs * s->heads > (1LL << 24))
-    return fail(PISA_UNSUPPORTED, "seqs * heads = %lld exceeds 2^24", (long long)s->seqs * s->heads);
+  if ((long long)s->seqs * s->heads >= (1LL << 24))        // a launch has below 2^32 threads
+    return fail(PISA_UNSUPPORTED, "seqs * heads = %lld is not below 2^24", (long long)s->seqs * s->heads);
   p->seqs = s->seqs;
   p->heads = s->heads;
   p->kv_heads = s->kv_heads;
@@ -250,7 +255,7 @@ int32_t pisa_paged_append(const pisa_paged_shape* shape, const void* k, const vo
   if ((tokens > 0 && (!k || !v)) || !offsets || !k_pages || !v_pages || !page_table || !lengths)
     return fail(PISA_INVALID_ARG, "k, v, offsets, k_pages, v_pages, page_table, lengths must not be NULL");
   PISA_CHECK_ALIGN(k, v, offsets, k_pages, v_pages, page_table, lengths);
-  if ((long long)tokens * p.kv_heads * p.d >= (1LL << 36)) return fail(PISA_UNSUPPORTED, "tensor too large");
+  if ((long long)tokens * p.kv_heads * p.d >= (1LL << 32)) return fail(PISA_UNSUPPORTED, "k and v must have below 2^32 elements");
   p.k = static_cast<unsigned char*>(k_pages);
   p.v = static_cast<unsigned char*>(v_pages);
   p.table = page_table;

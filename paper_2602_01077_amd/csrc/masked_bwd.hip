@@ -103,7 +103,7 @@ __device__ __forceinline__ void store_row(unsigned char* dst, const f32x16 (&acc
 }
 
 template <typename T, int D, int MOD>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(Masked p, Plan plan) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked_dq_kernel(Masked p, Plan plan) {
   using G = Geo<T, D>;
   constexpr int TILEB = G::TILEB, NDT = G::NDT;
   constexpr bool TIGHT = sizeof(T) == 2 && D == 128, ANEW = TIGHT || sizeof(T) == 4;
@@ -253,6 +253,31 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
     half(std::integral_constant<int, 32>{});
   };
   walk_stages<T>(t_begin, t_end, trip);
+  // Keys of inf or NaN in the tiles that were cleaned of them: their channels are NaN for the rows that see them.  The walk only
+  // remembers that there were any.
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(bad[0] | bad[1]) != 0u, 0))
+    for (int t = t_begin; t < t_end; ++t) {
+      if (covers(gs, t * kRows, kRows)) continue;
+      __syncthreads();
+      if (tid < 2) bad[tid] = 0u;
+      __syncthreads();
+      mark_rows<T, D>(kg + (long long)t * kRows * p.sk.token, p.sk.token, p.kv_len - t * kRows, (LDS_PTR(unsigned))&bad[0], tid);
+      __syncthreads();
+#pragma unroll 1
+      for (int r = 0; r < kRows; ++r) {
+        if (!((__builtin_amdgcn_readfirstlane(bad[r >> 5]) >> (r & 31)) & 1u)) continue;
+        const int key = t * kRows + r;
+        const T* src = reinterpret_cast<const T*>(kg + (long long)key * p.sk.token);
+        const bool mine = key >= iv.lo && key < iv.hi;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float x = (float)src[32 * dt + (e / 4) * 8 + 4 * h + e % 4];
+            acc[dt][e] = fmaf(mine ? x : 0.f, 0.f, acc[dt][e]);
+          }
+      }
+    }
   if constexpr (MENDS) {
     off += __shfl_xor(off, 32);
     delta += off;
@@ -292,7 +317,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dq_kernel(
 }
 
 template <typename T, int D, int MOD>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_dkv_kernel(Masked p, Plan plan) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked_dkv_kernel(Masked p, Plan plan) {
   using G = Geo<T, D>;
   constexpr int TILEB = G::TILEB, NDT = G::NDT;
   constexpr bool TIGHT = sizeof(T) == 2 && D == 128, ANEW = TIGHT || sizeof(T) == 4;

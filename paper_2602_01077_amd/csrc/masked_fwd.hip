@@ -91,11 +91,12 @@ __device__ __forceinline__ float weigh(const Score<T, MOD>& sc, const f32x16& s,
 }
 
 // The maximum is taken anew only where a sum of weights against the old one nears overflow (and on a wave's first tile, whose
-// old maximum is -inf): fp32 and bf16 share their exponents, so a stale maximum costs no digits.
-constexpr float kStaleLimit = 0x1p60f;
+// old maximum is -inf): fp32 and bf16 share their exponents, so a stale maximum costs no digits.  What it costs is range: values
+// have to stay this factor below the largest number.
+constexpr float kStaleLimit = 0x1p24f;
 
 template <typename T, int D, int MOD>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void masked_fwd_kernel(Masked p, Plan plan) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked_fwd_kernel(Masked p, Plan plan) {
   using G = Geo<T, D>;
   constexpr int TILEB = G::TILEB, NDT = G::NDT;
   __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * TILEB];      // K0 | K1 | V0 | V1
@@ -387,9 +388,10 @@ int parts_of(const Masked& m) {
     // Two tiles or more to a part; one where all parts still find a compute unit each (2 heads of 300 40 -> 25).
     parts = std::max(std::min(((m.d == 64 ? 64 : 96) + u - 1) / u, tiles / 2), std::min(32 / u, tiles));
   } else {
-    // whole rounds of the 32 compute units of an XCD, and about a tile's time for a part's own sums and its part in the joining
+    // whole rounds of the 32 compute units of an XCD, and about a tile's time for a part's own sums and its part in the joining;
+    // 512 parts an XCD at most, past which what a last round leaves idle is little
     long long best = 1LL << 60;
-    for (long long n = 1; n <= 16 && (n == 1 || n <= tiles / 2); ++n) {
+    for (long long n = 1; n <= 16 && (n == 1 || (n <= tiles / 2 && n * u <= 512)); ++n) {
       const long long rounds = (u * n + 31) / 32, cost = rounds * (tiles * 64 / n + 64);
       if (cost < best) {
         best = cost;

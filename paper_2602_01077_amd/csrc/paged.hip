@@ -167,6 +167,7 @@ __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(
   const unsigned lds_pages = (unsigned)(unsigned long long)(LDS_PTR(int32_t)) & pages[wave][0][0];
   const float unit_scale = sizeof(T) == 2 ? kLog2e : 1.f;
   const float to_cap = MOD & CAP ? p.scale / p.cap : p.scale * unit_scale, cap = p.cap * unit_scale;
+  const Near near(cap);
 
   for (long long x = x_begin; x < x_end;) {
     const int length = __builtin_amdgcn_readfirstlane(length_of(p, seq));
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(256, (PGeo<T, D>::GROUPS / 256)) void paged_kernel(
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float y = s[r] * to_cap;
-          if (MOD & CAP) y = cap * tanh_of<T>(y);
+          if (MOD & CAP) y = tanh_times<T>(y, near, cap);
           if (MOD & BIAS) y = fmaf(-slope, (float)(length - 1 - (key0 + i * P::TILE + 16 * sub + 4 * g + r)), y);
           if (!((bits >> (16 * sub + 4 * g + r)) & 1u)) y = -INFINITY;
           z[4 * sub + r] = y;

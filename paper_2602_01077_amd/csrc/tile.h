@@ -256,6 +256,12 @@ struct Near {                                    // mult tanh(x) = x of(x^2)
   __device__ __forceinline__ Near(float mult) : c0(mult * 9.999999019e-01f), c1(mult * -3.333136246e-01f), c2(mult * 1.327097675e-01f), c3(mult * -4.755360305e-02f) {}
   __device__ __forceinline__ float of(float u) const { return fmaf(fmaf(fmaf(c3, u, c2), u, c1), u, c0); }
 };
+// mult tanh(x) of one value, as cap_scores has it.
+template <typename T> __device__ __forceinline__ float tanh_times(float x, const Near& near, float mult) {
+  if (sizeof(T) == 4) return mult * tanhf(x);
+  const float far = fmaf(-2.f * mult, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f), mult);
+  return fabsf(x) <= kNear ? x * near.of(x * x) : far;
+}
 // s = mult tanh(to_cap s), to_cap > 0, for 32 rows' worth of scores.
 template <typename T> __device__ __forceinline__ void cap_scores(f32x16& s, float to_cap, float mult) {
   if (sizeof(T) == 4) {
@@ -276,19 +282,26 @@ template <typename T> __device__ __forceinline__ void cap_scores(f32x16& s, floa
     for (int r = 0; r < 16; ++r) s[r] *= near.of(s[r] * s[r]);
   } else {                                       // score by score, so that what a row gives does not hang on its neighbours
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float x = s[r];
-      const float far = fmaf(-2.f * mult, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f), mult);
-      s[r] = fabsf(x) <= kNear ? x * near.of(x * x) : far;
-    }
+    for (int r = 0; r < 16; ++r) s[r] = tanh_times<T>(s[r], near, mult);
   }
 }
-template <typename T> __device__ __forceinline__ float tanh_of(float x) {
-  if (sizeof(T) == 4) return tanhf(x);
-  return fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f), 1.f);
+// An element that is not finite, as its bits: infinity becomes the largest number, whose score is as far off and which a weight
+// of 0 takes away, NaN becomes 0.
+template <typename T> __device__ __forceinline__ unsigned tamed(unsigned w) {
+  if (sizeof(T) == 2) return (w & 0x7fu) ? 0u : (w & 0x8000u) | 0x7f7fu;
+  return (w & 0x7fffffu) ? 0u : (w & 0x80000000u) | 0x7f7fffffu;
 }
-
-// Non-finite elements of a staged tile are set to 0, and the rows they were in marked in bad[0..1] (64 bits, zero before).  A
+// Whether some element of these 16 bytes is infinite or NaN: its exponent is all ones.
+template <typename T> __device__ __forceinline__ bool unlike_finite(u32x4 w) {
+  unsigned top = 0u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    top = max(top, w[e] & 0x7f800000u);
+    if (sizeof(T) == 2) top = max(top, (w[e] & 0x7f80u) << 16);
+  }
+  return top == 0x7f800000u;
+}
+// Non-finite elements of a staged tile are tamed, and the rows they were in marked in bad[0..1] (64 bits, zero before).  A
 // product contracts over all rows of a tile, also where the weight is 0, and 0 * inf is NaN: tiles that are masked in part are
 // cleaned first.  All 256 threads; a barrier before and after is the caller's.
 template <typename T, int D> __device__ __forceinline__ void clean_tile(LDS_PTR(unsigned char) stage, LDS_PTR(unsigned) bad, int tid) {
@@ -298,28 +311,32 @@ template <typename T, int D> __device__ __forceinline__ void clean_tile(LDS_PTR(
     const int at = (i * 256 + tid) * 16;
     LDS_PTR(u32x4) p = reinterpret_cast<LDS_PTR(u32x4)>(stage + at);
     u32x4 w = *p;
-    unsigned found = 0;
+    if (unlike_finite<T>(w)) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (sizeof(T) == 2) {
-        if ((w[e] & 0x7f80u) == 0x7f80u) {
-          w[e] &= 0xffff0000u;
-          found = 1;
+      for (int e = 0; e < 4; ++e) {
+        if (sizeof(T) == 2) {
+          if ((w[e] & 0x7f80u) == 0x7f80u) w[e] = (w[e] & 0xffff0000u) | tamed<T>(w[e] & 0xffffu);
+          if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] = (w[e] & 0xffffu) | tamed<T>(w[e] >> 16) << 16;
+        } else if ((w[e] & 0x7f800000u) == 0x7f800000u) {
+          w[e] = tamed<T>(w[e]);
         }
-        if ((w[e] & 0x7f800000u) == 0x7f800000u) {
-          w[e] &= 0xffffu;
-          found = 1;
-        }
-      } else if ((w[e] & 0x7f800000u) == 0x7f800000u) {
-        w[e] = 0u;
-        found = 1;
       }
-    }
-    if (found) {
       *p = w;
       const int r = at / G::ROWB;
       atomicOr((unsigned*)(bad + (r >> 5)), 1u << (r & 31));
     }
+  }
+}
+
+// The same marks for 64 rows in memory, the first `avail` of them there.
+template <typename T, int D> __device__ __forceinline__ void mark_rows(const unsigned char* rows, long long stride, int avail,
+                                                                       LDS_PTR(unsigned) bad, int tid) {
+  using G = Geo<T, D>;
+  for (int i = 0; i < G::TILEB / 4096; ++i) {
+    const int at = (i * 256 + tid) * 16, r = at / G::ROWB;
+    if (r >= avail) continue;
+    const u32x4 w = *reinterpret_cast<const u32x4*>(rows + r * stride + at % G::ROWB);
+    if (unlike_finite<T>(w)) atomicOr((unsigned*)(bad + (r >> 5)), 1u << (r & 31));
   }
 }
 

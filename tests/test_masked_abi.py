@@ -171,3 +171,22 @@ def test_oracle_gradients_against_differences():
         u = rng.standard_normal((q, k, v)[which].shape)
         up, down = ([x + (s * 1e-6 * u if i == which else 0) for i, x in enumerate((q, k, v))] for s in (1, -1))
         assert abs((loss(up) - loss(down)) / 2e-6 - float((r[name] * u).sum())) < 1e-7
+
+
+@pytest.mark.parametrize("kw", [dict(softcap=2.0 ** -70), dict(softcap=2.0 ** 70), dict(softcap=1.0, scale=2.0 ** 100),
+                                dict(softcap=1.0, scale=2.0 ** -100)])
+def test_caps_whose_quotients_leave_the_range_are_refused(kw):
+    assert forward(masked(**kw)) == NOT_BUILT and "softcap" in pisa.last_error()
+    assert backward(masked(**kw)) == NOT_BUILT
+    assert decode(paged(**kw)) == NOT_BUILT and "softcap" in pisa.last_error()
+
+
+def test_launches_past_2_to_the_32_threads_are_refused():
+    dense = S(0, 0, 0)
+    big = dict(batch=1, heads=65535, kv_heads=1, q_len=128 * 256 + 1, kv_len=1, q=dense, k=dense, v=dense, out=dense)
+    assert forward(masked(**big)) == NOT_BUILT and "too large" in pisa.last_error()
+    s = paged()
+    rows = s.kv_heads * s.head_dim
+    assert append(s, tokens=(1 << 32) // rows) == NOT_BUILT
+    assert decode(paged(seqs=(1 << 24) // s.heads)) == NOT_BUILT
+    assert decode(paged(num_pages=(1 << 31) - 1, k_pages=S(1 << 39, 128, 256))) == NOT_BUILT

@@ -291,3 +291,169 @@ def test_without_masks_as_dense_attention(lib):
     bound = 2 * mo.forward_bounds(ref, 2.0 ** -7, n_terms(700, 128))
     assert np.all(np.abs(f64(a) - f64(b)) <= bound)
     assert (la - lb).abs().max() <= 2 * 2.0 ** -24 * n_terms(700, 128) * (1 + ref["zmax"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_seen_key_of_infinity_keeps_its_weight_of_zero(lib, dtype):
+    """A key whose infinite channel makes its score -inf for the rows that see it has weight 0 there, in tiles that are masked
+    in part as elsewhere: out, dk, dv and the finite channels of dq are those of a mask without it, its channel of dq is NaN
+    (0 * inf) for the rows that see it and finite for the others."""
+    n, key, ch = 100, 30, 7
+    q, k, v, dout = make(30, 1, 2, 2, n, n, 128, dtype)
+    q[..., ch] = -q[..., ch].abs() - 0.5
+    k[0, 0, key, ch] = float("inf")
+    out, lse = lib.masked_attention(q, k, v, causal=True, want_lse=True)
+    dq, dk, dv = lib.masked_attention_backward(q, k, v, out, lse, dout, causal=True)
+    torch.cuda.synchronize()
+    see = mo.visible(1, n, n, True)
+    see[:, :, key] = False
+    q, k, v, dout, out, dq, dk, dv = (x[:, :1] for x in (q, k, v, dout, out, dq, dk, dv))
+    scale = lib.resolved_scale(128)
+    ref = mo.attention(f64(q), f64(k), f64(v), see, scale, dout=f64(dout))
+    eps = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -23
+    assert np.all(np.abs(f64(out) - ref["out"]) <= mo.forward_bounds(ref, eps, n_terms(n, 128)))
+    bounds = mo.gradient_bounds(ref, eps, n_terms(n, 128), scale)
+    assert torch.isnan(dq[0, 0, key:, ch]).all()
+    dq[0, 0, key:, ch] = torch.from_numpy(ref["dq"][0, 0, key:, ch]).to(dq)
+    for name, got in (("dq", dq), ("dk", dk), ("dv", dv)):
+        assert np.all(np.abs(f64(got) - ref[name]) <= bounds[name]), name
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp32", 128), ("fp32", 64)])
+@pytest.mark.parametrize("seed", range(6))
+def test_drawn_calls(lib, seed, dtype, d):
+    """Sizes, masks, caps, slopes and orders drawn by seed."""
+    rng = np.random.default_rng([seed, d, dtype == "fp32"])
+    b, kvh, group = int(rng.integers(1, 3)), int(rng.integers(1, 4)), int(rng.integers(1, 5))
+    n = int(rng.integers(1, 400))
+    m = n if rng.random() < 0.5 else int(rng.integers(1, 700))
+    causal = bool(rng.random() < 0.6)
+    docs = prefix = None
+    if rng.random() < 0.7:                       # borders that leave padding before and behind, and may repeat
+        docs = [sorted(int(x) for x in rng.integers(0, m + 1, int(rng.integers(2, 9)))) for _ in range(b)]
+        docs = [x[:min(len(y) for y in docs)] for x in docs]
+    if causal and rng.random() < 0.6:            # below 0 and past the end as well
+        prefix = [[int(x) for x in rng.integers(-20, m + 50, 1 if docs is None else len(docs[0]) - 1)] for _ in range(b)]
+    softcap = float(rng.choice([0.0, 0.0, 8.0, 30.0]))
+    slopes = [float(x) for x in rng.random(kvh * group)] if rng.random() < 0.3 else None
+    print(b, kvh, group, n, m, causal, docs, prefix, softcap, slopes, flush=True)
+    q, k, v, dout = make(seed, b, kvh * group, kvh, n, m, d, dtype, tokens_first=bool(rng.random() < 0.5))
+    check(lib, q, k, v, dout, causal, docs, prefix, softcap, slopes)
+
+
+@pytest.mark.parametrize("dtype,softcap", [("bf16", 1e-3), ("bf16", 0.3), ("bf16", 1e6), ("fp32", 1e-3), ("fp32", 1e6)])
+def test_caps_of_any_size(lib, dtype, softcap):
+    # gradients for the large one only: 1 - tanh^2 of a capped score rounds to 0 or 2^-24, which has no relative bound
+    q, k, v, dout = make(31, 1, 2, 1, 140, 140, 64, dtype)
+    check(lib, q, k, v, dout, True, None, None, softcap, backward=softcap > 1)
+
+
+def test_heads_that_do_not_divide_by_the_xcds(lib):
+    q, k, v, dout = make(32, 1, 13, 13, 700, 700, 64, "bf16")
+    check(lib, q, k, v, dout, True, None, None)
+
+
+def test_more_documents_than_a_workgroup_keeps(lib):
+    rng = np.random.default_rng(33)
+    docs = [sorted(int(x) for x in rng.integers(0, 1501, 701)) for _ in range(2)]
+    q, k, v, dout = make(33, 2, 2, 1, 1500, 1500, 64, "bf16")
+    check(lib, q, k, v, dout, True, docs, [[int(x) for x in rng.integers(0, 4, 700)] for _ in range(2)])
+
+
+def test_more_tiles_than_are_ranked(lib):
+    """33 000 rows in documents; each document is a problem of its own, and three are compared."""
+    n, d = 33000, 64
+    borders = list(range(0, n, 977)) + [n]
+    q, k, v, dout = make(34, 1, 1, 1, n, n, d, "bf16")
+    args = dict(causal=True, doc_offsets=ints([borders]))
+    out, lse = lib.masked_attention(q, k, v, want_lse=True, **args)
+    grads = lib.masked_attention_backward(q, k, v, out, lse, dout, **args)
+    torch.cuda.synchronize()
+    scale, terms = lib.resolved_scale(d), n_terms(977, d)
+    for c in (0, len(borders) // 2, len(borders) - 2):
+        part = slice(borders[c], borders[c + 1])
+        size = borders[c + 1] - borders[c]
+        one = lambda x: f64(x[:, :, part])
+        ref = mo.attention(one(q), one(k), one(v), mo.visible(1, size, size, True), scale, dout=one(dout))
+        assert np.all(np.abs(one(out) - ref["out"]) <= mo.forward_bounds(ref, 2.0 ** -7, terms))
+        bounds = mo.gradient_bounds(ref, 2.0 ** -7, terms, scale)
+        for name, got in zip(("dq", "dk", "dv"), grads):
+            assert np.all(np.abs(one(got) - ref[name]) <= bounds[name]), name
+
+
+def test_tensors_past_4_gib(lib):
+    """Rows a MiB apart: offsets past 32 bits, the same bits as of dense tensors."""
+    n, d, apart = 4500, 128, 1 << 19
+    q, k, v, dout = make(35, 1, 2, 1, n, n, d, "bf16")
+    far = torch.empty(n, apart, dtype=torch.bfloat16, device=DEV)
+    slot = iter(range(0, apart, d))
+
+    def spread(heads, src=None):
+        at = [next(slot) for _ in range(heads)][0]
+        t = far[:, at:at + heads * d].view(n, heads, d).transpose(0, 1)[None]
+        return t if src is None else t.copy_(src)
+    fq, fk, fv, fg = spread(2, q), spread(1, k), spread(1, v), spread(2, dout)
+    out, lse = lib.masked_attention(q, k, v, causal=True, want_lse=True)
+    grads = lib.masked_attention_backward(q, k, v, out, lse, dout, causal=True)
+    fout, flse = lib.masked_attention(fq, fk, fv, causal=True, out=spread(2), want_lse=True)
+    fgrads = lib.masked_attention_backward(fq, fk, fv, fout, flse, fg, causal=True, dq=spread(2), dk=spread(1), dv=spread(1))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((out, lse, *grads), (fout, flse, *fgrads)))
+
+
+def test_one_row_for_all_heads(lib):
+    """Inputs expanded over batch and heads (strides of 0), with a single row as well."""
+    for n in (1, 70):
+        q, k, v, dout = make(36, 1, 1, 1, n, 90, 128, "bf16")
+        wide = [x.expand(2, 3, -1, -1) for x in (q, k, v, dout)]
+        dense = [x.contiguous() for x in wide]
+        out, lse = lib.masked_attention(*wide[:3], causal=True, want_lse=True)
+        ref, lse_ref = lib.masked_attention(*dense[:3], causal=True, want_lse=True)
+        got = lib.masked_attention_backward(*wide[:3], out, lse, wide[3], causal=True)
+        want = lib.masked_attention_backward(*dense[:3], ref, lse_ref, dense[3], causal=True)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((out, lse, *got), (ref, lse_ref, *want)))
+
+
+def test_two_graphs_with_one_workspace(lib):
+    """Replayed one after the other, in turn; and two calls at once, with a workspace each."""
+    calls = []
+    for seed, (h, n, m, dtype) in ((40, (2, 3, 2500, "bf16")), (41, (3, 300, 300, "fp32"))):
+        q, k, v, dout = make(seed, 1, h, 1, n, m, 64, dtype)
+        out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device=DEV)
+        calls.append((q, k, v, dout, out, lse, *(torch.empty_like(x) for x in (q, k, v))))
+    need = max(lib.masked_attention_workspace_bytes(*c[:3], causal=True, backward=x) for c in calls for x in (False, True))
+    shared = torch.empty(need, dtype=torch.uint8, device=DEV)
+
+    def step(c, ws):
+        q, k, v, dout, out, lse, dq, dk, dv = c
+        lib.masked_attention(q, k, v, causal=True, out=out, lse=lse, workspace=ws)
+        lib.masked_attention_backward(q, k, v, out, lse, dout, causal=True, dq=dq, dk=dk, dv=dv, workspace=ws)
+    for c in calls:
+        step(c, shared)
+    torch.cuda.synchronize()
+    want = [[x.clone() for x in c[4:]] for c in calls]
+    graphs = []
+    for c in calls:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step(c, shared)
+        graphs.append(g)
+    for _ in range(3):
+        for c, g in zip(calls, graphs):
+            for x in c[4:]:
+                x.fill_(float("nan"))
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for c, w in zip(calls, want) for a, b in zip(c[4:], w))
+    streams = [torch.cuda.Stream() for _ in calls]
+    for c in calls:
+        for x in c[4:]:
+            x.fill_(float("nan"))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                step(c, None)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for c, w in zip(calls, want) for a, b in zip(c[4:], w))

@@ -269,3 +269,51 @@ def test_graph_replays_follow_the_lengths(lib):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("softcap", [1e-3, 0.5, 1e6])
+def test_caps_of_any_size(lib, dtype, softcap):
+    lengths = [400, 3]
+    kp, vp, table, rows = cache(20, lengths, 2, 16, 64, dtype)
+    q = (1.5 * torch.randn(2, 4, 64, generator=torch.Generator().manual_seed(21))).to(DT[dtype]).to(DEV)
+    out, lse = lib.paged_attention(q, kp, vp, table, torch.tensor(lengths, dtype=torch.int32, device=DEV), softcap=softcap, want_lse=True)
+    torch.cuda.synchronize()
+    close(out, lse, oracle(q, rows, lengths, lib.resolved_scale(64), softcap), dtype, 400, 64)
+
+
+def test_sequences_that_share_pages(lib):
+    """Three sequences go on from the same pages."""
+    page, shared = 16, 48
+    kp, vp, table, rows = cache(22, [100], 2, page, 128, "bf16", spare=8)
+    free = sorted(set(range(kp.shape[0])) - set(table[0].tolist()))
+    tables = table.expand(3, -1).contiguous()
+    tables[1, 3], tables[2, 3] = free[0], free[1]
+    lengths, mine = [100, 60, 49], [rows[0]]
+    for s in (1, 2):
+        new = [torch.randn(lengths[s] - shared, 2, 128, generator=torch.Generator().manual_seed(s)).to(torch.bfloat16) for _ in range(2)]
+        mine.append([torch.cat([old[:shared], x]) for old, x in zip(rows[0], new)])
+        offsets = torch.tensor([0, 0, lengths[1] - shared if s == 1 else 0, lengths[s] - shared], dtype=torch.int32, device=DEV)
+        lib.paged_append(new[0].to(DEV), new[1].to(DEV), offsets, kp, vp, tables, torch.tensor(lengths, dtype=torch.int32, device=DEV))
+    q = torch.randn(3, 4, 128, generator=torch.Generator().manual_seed(23)).to(torch.bfloat16).to(DEV)
+    out, lse = lib.paged_attention(q, kp, vp, tables, torch.tensor(lengths, dtype=torch.int32, device=DEV), want_lse=True)
+    torch.cuda.synchronize()
+    close(out, lse, oracle(q, mine, lengths, lib.resolved_scale(128)), "bf16", 100, 128)
+
+
+def test_two_calls_at_once(lib):
+    calls = []
+    for seed, lengths in ((24, [3000, 5]), (25, [700] * 9)):
+        kp, vp, table, _ = cache(seed, lengths, 2, 32, 128, "bf16")
+        q = torch.randn(len(lengths), 8, 128, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16).to(DEV)
+        calls.append((q, kp, vp, table, torch.tensor(lengths, dtype=torch.int32, device=DEV)))
+    want = [lib.paged_attention(*c, want_lse=True) for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        got = []
+        for c, s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                got.append(lib.paged_attention(*c, want_lse=True))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
