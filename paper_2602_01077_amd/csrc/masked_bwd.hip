@@ -497,8 +497,16 @@ template <typename T, int D> __global__ __launch_bounds__(256) void masked_sum_k
   const int r = blockIdx.x * ROWS + tid / PER_ROW, ch = 4 * (tid % PER_ROW), row = unit % plan.deal.n_tiles * kOwn + r;
   if (row >= to.len) return;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < n_parts; ++i)
-    sum += *reinterpret_cast<const f32x4*>(plan.part + ((((size_t)unit * n_parts + i) * to.count + which) * kOwn + r) * D + ch);
+  const float* src = plan.part + (((size_t)unit * n_parts * to.count + which) * kOwn + r) * D + ch;
+  for (int i0 = 0; i0 < n_parts; i0 += 8) {      // eight parts under way at a time
+    f32x4 x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i0 + u < n_parts) x[u] = *reinterpret_cast<const f32x4*>(src + (size_t)(i0 + u) * to.count * kOwn * D);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i0 + u < n_parts) sum += x[u];
+  }
   const Strides& sd = to.stride[which];
   unsigned char* dst = to.at[which] + b * sd.batch + head * sd.head + (long long)row * sd.token;
   if constexpr (sizeof(T) == 2)

@@ -348,16 +348,35 @@ template <typename T, int D> __global__ __launch_bounds__(256) void masked_join_
   if (row >= p.q_len) return;
   const size_t item = (size_t)unit * n_parts;
   float m = -INFINITY, l = 0.f;
-  for (int i = 0; i < n_parts; ++i) m = fmaxf(m, plan.part_ml[((item + i) * 2) * kQRows + r]);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < n_parts; ++i) {
-    const float li = plan.part_ml[((item + i) * 2 + 1) * kQRows + r];
-    if (li == 0.f) continue;                     // no key of the row in this part
-    const float f = exp_of<T>(plan.part_ml[((item + i) * 2) * kQRows + r] - m);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(plan.part_o + ((item + i) * kQRows + r) * D + ch);
-    l += li * f;
+  for (int i0 = 0; i0 < n_parts; i0 += 8) {      // eight parts under way at a time
+    float mi[8], li[8];
+    f32x4 x[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += x[e] * f;
+    for (int u = 0; u < 8; ++u)
+      if (i0 + u < n_parts) {
+        mi[u] = plan.part_ml[((item + i0 + u) * 2) * kQRows + r];
+        li[u] = plan.part_ml[((item + i0 + u) * 2 + 1) * kQRows + r];
+        x[u] = *reinterpret_cast<const f32x4*>(plan.part_o + ((item + i0 + u) * kQRows + r) * D + ch);
+      }
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i0 + u < n_parts) top = fmaxf(top, mi[u]);
+    if (l != 0.f) {
+      const float f = exp_of<T>(m - top);
+      l *= f;
+      o *= f;
+    }
+    m = top;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i0 + u < n_parts && li[u] != 0.f) {    // 0: no key of the row in this part
+        const float f = exp_of<T>(mi[u] - m);
+        l += li[u] * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += x[u][e] * f;
+      }
   }
   const bool sees = l != 0.f;
   const float inv = sees ? 1.f / l : 0.f;
