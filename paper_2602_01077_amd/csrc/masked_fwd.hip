@@ -223,9 +223,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
     if (touches(ws, t * kRows, kRows)) {
       const float ahead = MOD & BIAS ? (float)(pos - t * kRows - 4 * h) : 0.f;
       const bool whole = covers(ws, t * kRows, kRows);
-      bool near = sizeof(T) == 2 && (MOD & CAP) && whole && sc.direct;
+      bool near = sizeof(T) == 2 && (MOD & CAP) && whole && sc.direct && i > 0;
       Weights<T> w0, w1;
-      float sum, top = 0.f;
+      float sum = INFINITY, top = 0.f;           // the first tile has no maximum to be weighed against
       if (near) {
         sum = weigh<T, MOD, true>(sc, s0, 1.f, sc.slope, -st.m, ahead, w0, top);
         sum += weigh<T, MOD, true>(sc, s1, 1.f, sc.slope, -st.m, ahead - 32.f, w1, top);
@@ -246,8 +246,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
             if ((unsigned)(at + key + 32) >= n) s1[r] = -INFINITY;
           }
         }
-        sum = weigh<T, MOD, false>(sc, s0, sc.c, sc.slope, -st.m, ahead, w0, top);
-        sum += weigh<T, MOD, false>(sc, s1, sc.c, sc.slope, -st.m, ahead - 32.f, w1, top);
+        if (i > 0) {
+          sum = weigh<T, MOD, false>(sc, s0, sc.c, sc.slope, -st.m, ahead, w0, top);
+          sum += weigh<T, MOD, false>(sc, s1, sc.c, sc.slope, -st.m, ahead - 32.f, w1, top);
+        }
       }
       if (__builtin_expect(__any(!(sum < kStaleLimit)), 0)) {
         // Row by row, so that what a row gives does not hang on its neighbours.  The scores are rounded as the maximum is taken
