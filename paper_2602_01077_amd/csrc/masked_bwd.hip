@@ -49,7 +49,7 @@ template <typename T, int MOD> struct Scorer {
   }
   // the weight exp(z - lse); `far` = pos - key; *gain = dz/ds
   __device__ __forceinline__ float weight(float s, float minus_lse, float far, float* gain) const {
-    *gain = MOD & CAP ? (1.f - s) * (1.f + s) : 1.f;
+    *gain = MOD & CAP ? __builtin_amdgcn_fmed3f(fmaf(-s, s, 1.f), 0.f, 1.f) : 1.f;       // within [0, 1] for s = -inf as well
     return exp_diff<T>(s, c, MOD & BIAS ? fmaf(-slope, fabsf(far), minus_lse) : minus_lse);
   }
 };
@@ -207,11 +207,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
       if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols), "+v"(lo));
       f32x16 s = rows_times<T, D, ROW0>(rd, k_off, q);
       sc.prepare(s);
-      const f32x16 dp = rows_times<T, D, ROW0>(rd, v_off, g);
+      f32x16 dp = rows_times<T, D, ROW0>(rd, v_off, g);
       phase<TIGHT>();
       Weights<T> w;
-      const unsigned n = (unsigned)(iv.hi - iv.lo);
       const int key0 = t * kRows + ROW0 + 4 * h;
+      if (part) {                                // masked keys: score -inf, nothing of v
+        asm volatile("");                        // a branch: selects for every tile took a quarter of the walk's plain operations
+        const unsigned n = (unsigned)(iv.hi - iv.lo);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if ((unsigned)(key0 + (r / 4) * 8 + r % 4 - lo) >= n) {
+            s[r] = -INFINITY;
+            dp[r] = 0.f;
+          }
+      }
       const float ahead = (float)(pos - key0);
       float top = 0.f;
 #pragma unroll
@@ -219,11 +228,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
         float x[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const int key = key0 + ((r + u) / 4) * 8 + (r + u) % 4;
           float gain;
-          float wt = sc.weight(s[r + u], minus_lse, ahead - (float)(((r + u) / 4) * 8 + (r + u) % 4), &gain);
+          const float wt = sc.weight(s[r + u], minus_lse, ahead - (float)(((r + u) / 4) * 8 + (r + u) % 4), &gain);
           x[u] = wt * (dp[r + u] - delta);
-          if (part && (unsigned)(key - lo) >= n) wt = x[u] = 0.f;
           if (MENDS) {
             off += x[u];
             top = fmaxf(top, wt);
@@ -238,7 +245,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
           const int key = key0 + (r / 4) * 8 + r % 4;
           float gain;
           const float wt = sc.weight(s[r], minus_lse, ahead - (float)((r / 4) * 8 + r % 4), &gain);
-          if (wt >= kHeavy && (unsigned)(key - lo) < n && n_heavy < kMostHeavy) {
+          if (wt >= kHeavy && (unsigned)(key - lo) < (unsigned)(iv.hi - iv.lo) && n_heavy < kMostHeavy) {
             heavy[n_heavy][tid].key = key;
             heavy[n_heavy][tid].weight = wt * gain;
             ++n_heavy;
@@ -427,39 +434,46 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
       if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols));
       f32x16 s = rows_times<T, D, ROW0>(rd, q_off, k);
       sc.prepare(s);
-      const f32x16 dp = rows_times<T, D, ROW0>(rd, g_off, v);
+      f32x16 dp = rows_times<T, D, ROW0>(rd, g_off, v);
       phase<TIGHT>();
       Weights<T> wp, wd;
       const int ln = TIGHT ? lane_anew() : lane, h = ln >> 5, own = 32 * wave + (ln & 31);   // own: this lane's key of the tile
-      int lo = 0;
-      unsigned count = 0u;
-      if (part) {
-        lo = seen_s[own].lo;
-        count = (unsigned)(seen_s[own].hi - lo);
-      }
       const int row0 = x0 + ROW0 + 4 * h;
       const float ahead = (float)(row0 + shift - (kt * kOwn + own));
+      auto stat4 = [&](int which, int e) INLINE {
+        return *reinterpret_cast<LDS_PTR(const f32x4)>((LDS_PTR(const float))&stat[par][which][ROW0 + 8 * e + 4 * h]);
+      };
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const f32x4 ml = *reinterpret_cast<LDS_PTR(const f32x4)>((LDS_PTR(const float))&stat[par][0][ROW0 + 8 * e + 4 * h]);
-        const f32x4 de = *reinterpret_cast<LDS_PTR(const f32x4)>((LDS_PTR(const float))&stat[par][1][ROW0 + 8 * e + 4 * h]);
-        float x[4], y[4];
+        const f32x4 ml = stat4(0, e), de = stat4(1, e);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const int r = 4 * e + u, row = row0 + 8 * e + u;
+          const int r = 4 * e + u;
           float gain;
-          x[u] = sc.weight(s[r], ml[u], ahead + (float)(8 * e + u), &gain);
-          y[u] = x[u] * (dp[r] - de[u]);
-          if (MOD & CAP) y[u] *= gain;
-          if (part) {
-            x[u] = fmaf(0.f, de[u], x[u]);       // a row of dout that was cleaned of inf or NaN has a delta of NaN
-            if ((unsigned)(row - lo) >= count) x[u] = y[u] = 0.f;
+          s[r] = sc.weight(s[r], ml[u], ahead + (float)(8 * e + u), &gain);
+          dp[r] = s[r] * (dp[r] - de[u]);
+          if (MOD & CAP) dp[r] *= gain;
+        }
+      }
+      if (part) {
+        asm volatile("");                        // a branch, as in masked_dq_kernel
+        const int lo = seen_s[own].lo;
+        const unsigned count = (unsigned)(seen_s[own].hi - lo);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 de = stat4(1, e);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int r = 4 * e + u;
+            s[r] = fmaf(0.f, de[u], s[r]);       // a row of dout that was cleaned of inf or NaN has a delta of NaN
+            if ((unsigned)(row0 + 8 * e + u - lo) >= count) s[r] = dp[r] = 0.f;
           }
         }
-        wp.set(4 * e, x[0], x[1]);
-        wp.set(4 * e + 2, x[2], x[3]);
-        wd.set(4 * e, y[0], y[1]);
-        wd.set(4 * e + 2, y[2], y[3]);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        wp.set(r, s[r], s[r + 1]);
+        wd.set(r, dp[r], dp[r + 1]);
       }
       phase<TIGHT>();
       cols_times<T, D, ROW0>(rd, g_off, wp, dv);
