@@ -106,7 +106,6 @@ template <typename T, int D, int MOD>
 __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked_dq_kernel(Masked p, Plan plan) {
   using G = Geo<T, D>;
   constexpr int TILEB = G::TILEB, NDT = G::NDT;
-  constexpr bool TIGHT = sizeof(T) == 2 && D == 128, ANEW = TIGHT || sizeof(T) == 4;
   __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * TILEB];      // K0 | V0 | K1 | V1
   constexpr bool MENDS = sizeof(T) == 2;
   __shared__ int span_s[4][4];
@@ -137,7 +136,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
   const unsigned char* kg = p.k + b * p.sk.batch + (head / p.group) * p.sk.head;
   const unsigned char* vg = p.v + b * p.sv.batch + (head / p.group) * p.sv.head;
   const unsigned lds = (unsigned)(unsigned long long)(LDS_PTR(unsigned char)) & stage[0];
-  Loader<T, D, ANEW> lk, lv;
+  Loader<T, D, sizeof(T) == 4> lk, lv;
   lk.init(wave, lane, (unsigned)p.sk.token);
   lv.init(wave, lane, (unsigned)p.sv.token);
   Reader<T, D> rd;
@@ -203,12 +202,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
     const bool part = !covers(ws, t * kRows, kRows);
     auto half = [&](auto row0_tag) INLINE {
       constexpr int ROW0 = decltype(row0_tag)::value;
-      int lo = iv.lo;                            // addresses and key numbers are made anew, see masked_dkv_kernel
-      if (TIGHT) asm volatile("" : "+v"(rd.rows), "+v"(rd.cols), "+v"(lo));
       f32x16 s = rows_times<T, D, ROW0>(rd, k_off, q);
       sc.prepare(s);
       f32x16 dp = rows_times<T, D, ROW0>(rd, v_off, g);
-      phase<TIGHT>();
       Weights<T> w;
       const int key0 = t * kRows + ROW0 + 4 * h;
       if (part) {                                // masked keys: score -inf, nothing of v
@@ -216,7 +212,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
         const unsigned n = (unsigned)(iv.hi - iv.lo);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if ((unsigned)(key0 + (r / 4) * 8 + r % 4 - lo) >= n) {
+          if ((unsigned)(key0 + (r / 4) * 8 + r % 4 - iv.lo) >= n) {
             s[r] = -INFINITY;
             dp[r] = 0.f;
           }
@@ -245,18 +241,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
           const int key = key0 + (r / 4) * 8 + r % 4;
           float gain;
           const float wt = sc.weight(s[r], minus_lse, ahead - (float)((r / 4) * 8 + r % 4), &gain);
-          if (wt >= kHeavy && (unsigned)(key - lo) < (unsigned)(iv.hi - iv.lo) && n_heavy < kMostHeavy) {
+          if (wt >= kHeavy && (unsigned)(key - iv.lo) < (unsigned)(iv.hi - iv.lo) && n_heavy < kMostHeavy) {
             heavy[n_heavy][tid].key = key;
             heavy[n_heavy][tid].weight = wt * gain;
             ++n_heavy;
           }
         }
       }
-      phase<TIGHT>();
       cols_times<T, D, ROW0>(rd, k_off, w, acc);
     };
     half(std::integral_constant<int, 0>{});
-    phase<TIGHT>();
     half(std::integral_constant<int, 32>{});
   };
   walk_stages<T>(t_begin, t_end, trip);
