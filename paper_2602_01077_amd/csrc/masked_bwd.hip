@@ -7,6 +7,10 @@
 //     dk, dv walk (a lane holds one key):    S = Q K^T,    dP = dO V^T,    dV^T += dO^T P,  dK^T += Q^T dS
 // so that P and dS leave the first products in the lanes in which the second ones take them.  The dk, dv walk goes over the
 // rows of all query heads that share the key head.
+//
+// Bound as the forward pass is, by operands from LDS and the plain operations between the products: 12 heads of 8 192, causal,
+// dq 367 us, dk and dv 448 (matrix cores 55 and 49 % busy); 24 heads of 4 608 without a mask 906 us together, 1 010 TFLOP/s over
+// the seven products.  At 64 channels with capped and biased scores, 2 x 12 heads of 2 777, 111 and 97 us (20 and 27 %).
 #include <algorithm>
 
 #include "masked.h"
