@@ -131,7 +131,8 @@ template <typename T, int D> struct Reader {
       static_assert(sizeof(T) == 4 || swz<T, D>(8) == 1, "row r + 8 lies at row r's chunk XOR 1");
       cols = tile + kq * G::ROWB + (((2 * lhalf + ((j & 3) >> 1)) ^ swz<T, D>(kq)) << 4) + 8 * (j & 1);
     } else {
-      cols = tile + 4 * h * G::ROWB + (lam & 3) * 4;
+      // swz(row + 4 h) is swz(row) ^ (h << 3) for the rows that this lane starts from, and XOR of chunks is XOR of addresses
+      cols = tile + 4 * h * G::ROWB + (lam & 3) * 4 + (((lam >> 2) ^ (h << 3)) << 4);
     }
   }
 };
@@ -152,13 +153,29 @@ template <typename T> __device__ __forceinline__ f32x16 mma_step(u32x4 a, u32x4 
   }
 }
 
+// fp32: what the next step takes from LDS is under way before this one's products.  Without it every read was waited for (the
+// scheduler moves reads to their use), and the matrix cores idle a third of the time.
+__device__ __forceinline__ void read_ahead() { __builtin_amdgcn_sched_barrier(0); }
+
 // acc = (32 rows of the tile, from row ROW0) * (the lane's own row, all channels).  OFF: byte offset of the tile.
 template <typename T, int D, int ROW0>
 __device__ __forceinline__ f32x16 rows_times(const Reader<T, D>& rd, unsigned off, const u32x4 (&b)[Geo<T, D>::STEPS]) {
   f32x16 acc = (f32x16){0};
+  if constexpr (sizeof(T) == 2) {
 #pragma unroll
-  for (int s = 0; s < Geo<T, D>::STEPS; ++s)
-    acc = mma_step<T>(lds_read<u32x4>((rd.rows ^ (s << 5)) + off + ROW0 * Geo<T, D>::ROWB), b[s], acc);
+    for (int s = 0; s < Geo<T, D>::STEPS; ++s)
+      acc = mma_step<T>(lds_read<u32x4>((rd.rows ^ (s << 5)) + off + ROW0 * Geo<T, D>::ROWB), b[s], acc);
+  } else {
+    unsigned at = rd.rows + off;                 // opaque: addresses kept for the walk would take the registers of what is read ahead
+    asm volatile("" : "+v"(at));
+    u32x4 a[2] = {lds_read<u32x4>(at + ROW0 * Geo<T, D>::ROWB)};
+#pragma unroll
+    for (int s = 0; s < Geo<T, D>::STEPS; ++s) {
+      if (s + 1 < Geo<T, D>::STEPS) a[(s + 1) & 1] = lds_read<u32x4>((at ^ ((s + 1) << 5)) + ROW0 * Geo<T, D>::ROWB);
+      read_ahead();
+      acc = mma_step<T>(a[s & 1], b[s], acc);
+    }
+  }
   return acc;
 }
 
@@ -202,16 +219,22 @@ __device__ __forceinline__ void cols_times(const Reader<T, D>& rd, unsigned off,
                                                           0, 0, 0);
       }
   } else {
-    const int h = (threadIdx.x >> 5) & 1, c = (threadIdx.x & 31) >> 2;
+    constexpr int N = Geo<T, D>::NDT;
+    unsigned at = rd.cols + off;
+    asm volatile("" : "+v"(at));
+    float a[2][N];
+    auto read = [&](int r) INLINE {
+      const int base = (r / 4) * 8 + r % 4;      // this lane reads row base + 4 h
+#pragma unroll
+      for (int dt = 0; dt < N; ++dt) a[r & 1][dt] = lds_read<float>((at ^ (unsigned)(((8 * (dt & 1)) ^ swz<T, D>(base)) << 4)) + 256 * (dt >> 1) + (ROW0 + base) * ROWB);
+    };
+    read(0);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int base = (r / 4) * 8 + r % 4;      // this lane reads row base + 4 h
-      const unsigned z = (unsigned)(swz<T, D>(base) ^ (h << 3));       // swz(base + 4 h): bit 2 of the row is bit 3 of the swizzle
+      if (r + 1 < 16) read(r + 1);
+      read_ahead();
 #pragma unroll
-      for (int dt = 0; dt < Geo<T, D>::NDT; ++dt) {
-        const float a = lds_read<float>(rd.cols + off + (ROW0 + base) * ROWB + (((8 * dt + c) ^ z) << 4));
-        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.w[r], acc[dt], 0, 0, 0);
-      }
+      for (int dt = 0; dt < N; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[r & 1][dt], p.w[r], acc[dt], 0, 0, 0);
     }
   }
 }
