@@ -16,8 +16,8 @@ ITERATIVE = ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"]
 # The kernel for four workgroups on a CU has 128 registers a lane: the iterative scheduler spills 30 of them in its walk
 # (half as slow again), the default and ILP ones a few, this one none.
 FOUR = ["-DPISA_ATTN_FOUR", "-mllvm", "-amdgpu-sched-strategy=max-memory-clause"]
-# The fp32 kernels of masked attention are compiled apart from the bf16 ones: one wave on a SIMD, they gain 12 % from the
-# iterative scheduler (8 heads of 4 500, causal, 562 -> 488 us), which spills the bf16 backward pass (1 200 -> 1 850).
+# The fp32 kernels of masked attention are compiled apart from the bf16 ones: they gain 2 % from the iterative scheduler (8 heads
+# of 4 500, 790 -> 776 us), which spills the bf16 backward pass (1 200 -> 1 850).
 F32 = ["-DPISA_MASKED_F32"] + ITERATIVE
 UNITS = [("api.hip", "api", []), ("stats.hip", "stats", []), ("stats_bf16.hip", "stats_bf16", []),
          ("select.hip", "select", []), ("hetero.hip", "hetero", []), ("attn_fp32.hip", "attn_fp32", []),
