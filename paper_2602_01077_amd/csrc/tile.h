@@ -153,18 +153,30 @@ template <typename T> __device__ __forceinline__ f32x16 mma_step(u32x4 a, u32x4 
   }
 }
 
-// fp32: what the next step takes from LDS is under way before this one's products.  Without it every read was waited for (the
-// scheduler moves reads to their use), and the matrix cores idle a third of the time.
-__device__ __forceinline__ void read_ahead() { __builtin_amdgcn_sched_barrier(0); }
+// What later steps take from LDS is under way before this one's products: three steps in bf16, one in fp32 (four instructions of
+// twice the time).  Left to itself the scheduler moves reads to their use and waits for each (24 heads of 4 608, backward 915 us,
+// so 888; fp32, 8 of 4 500, forward 895, so 776).  At 64 channels, where registers are left, plain operations may pass (24 of
+// 4 608 forward 171 where they may not, 159 so; at 128 channels 253 and 258).
+constexpr int kAhead = 3;
+template <typename T, int D> __device__ __forceinline__ void read_ahead() {
+  constexpr int kVector = 0x2, kScalar = 0x4, kTranscendental = 0x400;
+  __builtin_amdgcn_sched_barrier(sizeof(T) == 2 && D == 64 ? kVector | kScalar | kTranscendental : 0);
+}
 
 // acc = (32 rows of the tile, from row ROW0) * (the lane's own row, all channels).  OFF: byte offset of the tile.
 template <typename T, int D, int ROW0>
 __device__ __forceinline__ f32x16 rows_times(const Reader<T, D>& rd, unsigned off, const u32x4 (&b)[Geo<T, D>::STEPS]) {
   f32x16 acc = (f32x16){0};
   if constexpr (sizeof(T) == 2) {
+    constexpr int STEPS = Geo<T, D>::STEPS;
+    u32x4 a[STEPS];
 #pragma unroll
-    for (int s = 0; s < Geo<T, D>::STEPS; ++s)
-      acc = mma_step<T>(lds_read<u32x4>((rd.rows ^ (s << 5)) + off + ROW0 * Geo<T, D>::ROWB), b[s], acc);
+    for (int s = -kAhead; s < STEPS; ++s) {
+      if (s + kAhead < STEPS) a[s + kAhead] = lds_read<u32x4>((rd.rows ^ ((s + kAhead) << 5)) + off + ROW0 * Geo<T, D>::ROWB);
+      if (s < 0) continue;
+      read_ahead<T, D>();
+      acc = mma_step<T>(a[s], b[s], acc);
+    }
   } else {
     unsigned at = rd.rows + off;                 // opaque: addresses kept for the walk would take the registers of what is read ahead
     asm volatile("" : "+v"(at));
@@ -172,7 +184,7 @@ __device__ __forceinline__ f32x16 rows_times(const Reader<T, D>& rd, unsigned of
 #pragma unroll
     for (int s = 0; s < Geo<T, D>::STEPS; ++s) {
       if (s + 1 < Geo<T, D>::STEPS) a[(s + 1) & 1] = lds_read<u32x4>((at ^ ((s + 1) << 5)) + ROW0 * Geo<T, D>::ROWB);
-      read_ahead();
+      read_ahead<T, D>();
       acc = mma_step<T>(a[s & 1], b[s], acc);
     }
   }
@@ -204,20 +216,25 @@ template <typename T, int D, int ROW0>
 __device__ __forceinline__ void cols_times(const Reader<T, D>& rd, unsigned off, const Weights<T>& p, f32x16 (&acc)[Geo<T, D>::NDT]) {
   constexpr int ROWB = Geo<T, D>::ROWB;
   if constexpr (sizeof(T) == 2) {
+    constexpr int NDT = Geo<T, D>::NDT, N = 2 * NDT;
+    u32x4 a[N];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int dt = 0; dt < Geo<T, D>::NDT; ++dt) {
+    for (int i = -kAhead; i < N; ++i) {
+      if (i + kAhead < N) {
+        const int s = (i + kAhead) / NDT, dt = (i + kAhead) % NDT;
         const unsigned at = off + (ROW0 + 16 * s) * ROWB;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             reinterpret_cast<LDS_PTR(s16x4)>((LDS_PTR(unsigned char))(unsigned long long)((rd.cols ^ (dt << 6)) + at)));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             reinterpret_cast<LDS_PTR(s16x4)>((LDS_PTR(unsigned char))(unsigned long long)((rd.cols ^ (dt << 6) ^ 16) + at + 8 * ROWB)));
         const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
-        const u32x4 a = {l2.x, l2.y, h2.x, h2.y};
-        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, p.w[s]), acc[dt],
-                                                          0, 0, 0);
+        a[i + kAhead] = u32x4{l2.x, l2.y, h2.x, h2.y};
       }
+      if (i < 0) continue;
+      read_ahead<T, D>();
+      acc[i % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]), __builtin_bit_cast(bf16x8, p.w[i / NDT]),
+                                                             acc[i % NDT], 0, 0, 0);
+    }
   } else {
     constexpr int N = Geo<T, D>::NDT;
     unsigned at = rd.cols + off;
@@ -232,7 +249,7 @@ __device__ __forceinline__ void cols_times(const Reader<T, D>& rd, unsigned off,
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       if (r + 1 < 16) read(r + 1);
-      read_ahead();
+      read_ahead<T, D>();
 #pragma unroll
       for (int dt = 0; dt < N; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[r & 1][dt], p.w[r], acc[dt], 0, 0, 0);
     }
