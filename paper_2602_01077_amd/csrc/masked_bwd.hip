@@ -24,8 +24,8 @@ namespace {
 
 constexpr int kOwn = 128;                // rows (keys) of a workgroup, 32 to a wave
 constexpr int CAP = 1, BIAS = 2;         // bits of MOD
-constexpr float kHeavy = 0.1875f;        // see masked_dq_kernel
-constexpr int kMostHeavy = 5;            // weights of a row that can be as large
+constexpr float kHeavy = 0.1f;           // see masked_dq_kernel
+constexpr int kMostHeavy = 10;           // weights of a row that can be as large
 
 struct Plan {
   Deal deal;           // of tiles of 128 rows (dq), or keys (dk, dv) and the parts of their rows
@@ -114,10 +114,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
   constexpr bool MENDS = sizeof(T) == 2;
   __shared__ int span_s[4][4];
   __shared__ unsigned bad[2];
-  __shared__ struct {
-    int key;
-    float weight;                                // times dz/ds
-  } heavy[MENDS ? kMostHeavy : 1][MENDS ? 256 : 1];      // by thread: of its row, keys with its h
+  // by thread: of its row, keys with its h; weight times dz/ds in 255ths (it multiplies a correction), above a key below 2^24
+  __shared__ unsigned heavy[MENDS ? kMostHeavy : 1][MENDS ? 256 : 1];
 
   __shared__ int32_t docs_s[kDocsInLds + 1];
   __shared__ int size_s[kRankedTiles + 1];
@@ -246,8 +244,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
           float gain;
           const float wt = sc.weight(s[r], minus_lse, ahead - (float)((r / 4) * 8 + r % 4), &gain);
           if (wt >= kHeavy && (unsigned)(key - iv.lo) < (unsigned)(iv.hi - iv.lo) && n_heavy < kMostHeavy) {
-            heavy[n_heavy][tid].key = key;
-            heavy[n_heavy][tid].weight = wt * gain;
+            heavy[n_heavy][tid] = (unsigned)fminf(fmaf(wt * gain, 255.f, 0.5f), 255.f) << 24 | (unsigned)key;
             ++n_heavy;
           }
         }
@@ -293,8 +290,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
       for (int e = 0; __any(e < counts[half]); ++e)
         if (e < counts[half]) {
           const int of = (tid & ~32) + 32 * half;
-          const T* src = reinterpret_cast<const T*>(kg + (long long)heavy[e][of].key * p.sk.token);
-          const float f = -off * heavy[e][of].weight;
+          const unsigned entry = heavy[e][of];
+          const T* src = reinterpret_cast<const T*>(kg + (long long)(entry & 0xffffffu) * p.sk.token);
+          const float f = -off * ((float)(entry >> 24) * (1.f / 255.f));
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
