@@ -9,8 +9,8 @@
 // rows of all query heads that share the key head.
 //
 // Bound as the forward pass is, by operands from LDS and the plain operations between the products: 12 heads of 8 192, causal,
-// dq 367 us, dk and dv 448 (matrix cores 55 and 49 % busy); 24 heads of 4 608 without a mask 906 us together, 1 010 TFLOP/s over
-// the seven products.  At 64 channels with capped and biased scores, 2 x 12 heads of 2 777, 111 and 97 us (20 and 27 %).
+// dq 340 us, dk and dv 407 (matrix cores 60 and 56 % busy); 24 heads of 4 608 without a mask 890 us together, 1 025 TFLOP/s over
+// the seven products.  At 64 channels with capped and biased scores, 2 x 12 heads of 2 777, 112 and 96 us (20 and 27 %).
 #include <algorithm>
 
 #include "masked.h"

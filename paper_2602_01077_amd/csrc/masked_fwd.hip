@@ -8,10 +8,10 @@
 // those that none of its rows sees, and compares key numbers only in those that some of them see in part.
 //
 // Bound (bf16, 128 channels) by operands from LDS, 1 KB to a matrix instruction, which is the LDS rate itself, and by the softmax
-// beside it: 24 heads of 4 608 tokens without a mask 255 us, 1 020 TFLOP/s; causal, 12 of 8 192, 225 us, matrix cores 57 % busy.
+// beside it: 24 heads of 4 608 tokens without a mask 255 us, 1 020 TFLOP/s; causal, 12 of 8 192, 222 us, matrix cores 58 % busy.
 // 32 rows a wave leave room for two waves on a SIMD, of which one is in its softmax while the other multiplies.  64 channels with
 // capped and biased scores are bound by vector instructions (2 x 12 heads of 2 777 70 us), fp32 by its matrix instruction (8 heads
-// of 4 500, causal, 486 us, 62 % busy).
+// of 4 500, causal, 417 us, 72 % busy).
 #include <algorithm>
 
 #include "masked.h"

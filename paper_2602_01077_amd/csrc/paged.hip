@@ -10,7 +10,7 @@
 // the columns of S^T = K Q^T and O^T = V^T P^T; register r of lane (j, g) holds key 4 g + r and column j, and that order of
 // the keys serves the second product as it stands.
 //
-// Measured: 48 sequences of up to 8 000 tokens, 32 / 8 heads, 165 us (5.2 TB/s); 2 of 200 000, 40 / 8 heads, 255 us (6.0 TB/s).
+// Measured: 48 sequences of up to 8 000 tokens, 32 / 8 heads, 167 us (5.1 TB/s); 2 of 200 000, 40 / 8 heads, 255 us (6.0 TB/s).
 #include "paged.h"
 #include "tile.h"
 
