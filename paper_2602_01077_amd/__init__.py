@@ -349,6 +349,8 @@ def _strides(size, stride, name: str) -> PisaStrides:
     """Of a [batch, heads, tokens, head_dim] view; the channels of a row have to lie together."""
     if stride[3] != 1 and size[3] > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
+    if stride[2] == 0 and size[2] > 1:           # with batch and head strides of 0 the library would take it for a dense tensor
+        raise ValueError(f"{name}: one row cannot stand for all tokens (a stride of 0)")
     return PisaStrides(stride[0], stride[1], stride[2] if size[2] > 1 else max(stride[2], size[3]))
 
 

@@ -190,3 +190,24 @@ def test_launches_past_2_to_the_32_threads_are_refused():
     assert append(s, tokens=(1 << 32) // rows) == NOT_BUILT
     assert decode(paged(seqs=(1 << 24) // s.heads)) == NOT_BUILT
     assert decode(paged(num_pages=(1 << 31) - 1, k_pages=S(1 << 39, 128, 256))) == NOT_BUILT
+
+
+@pytest.mark.parametrize("which", ["q", "k", "v", "out", "dout"])
+def test_one_row_for_all_tokens_is_refused(which):
+    """Expanded over batch, heads and tokens all strides are 0, which the library reads as dense: far past the one row that is there."""
+    t = {x: torch.zeros(2, 3, 70, 64) for x in ("q", "k", "v", "out", "dout")}
+    t[which] = torch.zeros(1, 1, 1, 64).expand(2, 3, 70, 64)
+    with pytest.raises(ValueError, match=f"{which}: one row"):
+        if which != "dout":
+            pisa.masked_attention(t["q"], t["k"], t["v"], out=t["out"])
+        pisa.masked_attention_backward(t["q"], t["k"], t["v"], t["out"], torch.zeros(2, 3, 70), t["dout"])
+
+
+def test_one_slot_for_a_whole_page_is_refused():
+    table, lengths = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    pages, one = torch.zeros(4, 16, 2, 64), torch.zeros(1, 1, 1, 64).expand(4, 16, 2, 64)
+    for k, v, name in ((one, pages, "k_pages"), (pages, one, "v_pages")):
+        with pytest.raises(ValueError, match=f"{name}: one row"):
+            pisa.paged_attention(torch.zeros(2, 4, 64), k, v, table, lengths)
+        with pytest.raises(ValueError, match=f"{name}: one row"):
+            pisa.paged_append(torch.zeros(3, 2, 64), torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int32), k, v, table, lengths)
