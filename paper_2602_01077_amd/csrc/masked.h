@@ -52,7 +52,7 @@ __device__ inline bool document_of(const Masked& m, const int32_t* offs, int pos
   }
   int lo = 0, hi = m.n_docs + 1;                  // the last offset <= pos is number lo - 1
   while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
+    const int mid = (int)(((unsigned)lo + (unsigned)hi) >> 1);      // the sum passes 31 bits from 2^30 documents on
     if (offs[mid] <= pos) lo = mid + 1;
     else hi = mid;
   }

@@ -457,3 +457,19 @@ def test_two_graphs_with_one_workspace(lib):
                 step(c, None)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for c, w in zip(calls, want) for a, b in zip(c[4:], w))
+
+
+def test_more_documents_than_30_bits_count(lib):
+    """Empty documents without end ahead of two that hold tokens: the search for a row's document passes 2^30 of them."""
+    n = 130
+    q, k, v, dout = make(50, 1, 2, 1, n, n, 64, "bf16")
+    short = ints([[0, 70, n]])
+    borders = torch.zeros(1, (1 << 30) + 100, dtype=torch.int32, device=DEV)
+    borders[0, -3:] = short[0]
+
+    def step(docs):
+        out, lse = lib.masked_attention(q, k, v, causal=True, doc_offsets=docs, want_lse=True)
+        return (out, lse, *lib.masked_attention_backward(q, k, v, out, lse, dout, causal=True, doc_offsets=docs))
+    want, got = step(short), step(borders)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
