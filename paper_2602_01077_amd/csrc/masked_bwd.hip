@@ -88,6 +88,12 @@ template <typename T> __device__ __forceinline__ float dot16(u32x4 a, u32x4 b) {
   return d;
 }
 
+template <typename T> __device__ __forceinline__ f32x4 four_of(const unsigned char* src) {      // elements that lie together
+  if constexpr (sizeof(T) == 4) return *reinterpret_cast<const f32x4*>(src);
+  const u32x2 x = *reinterpret_cast<const u32x2*>(src);
+  return f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u), __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xffff0000u)};
+}
+
 // The lane's row of sums, times f; zeros unless `some` (the sums of a row that has none can hold anything).
 template <typename T, int D>
 __device__ __forceinline__ void store_row(unsigned char* dst, const f32x16 (&acc)[Geo<T, D>::NDT], float f, bool some, int h) {
@@ -456,15 +462,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
         const int lo = seen_s[own].lo;
         const unsigned count = (unsigned)(seen_s[own].hi - lo);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const f32x4 de = stat4(1, e);
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int r = 4 * e + u;
-            s[r] = fmaf(0.f, de[u], s[r]);       // a row of dout that was cleaned of inf or NaN has a delta of NaN
-            if ((unsigned)(row0 + 8 * e + u - lo) >= count) s[r] = dp[r] = 0.f;
-          }
-        }
+        for (int r = 0; r < 16; ++r)
+          if ((unsigned)(row0 + (r / 4) * 8 + r % 4 - lo) >= count) s[r] = dp[r] = 0.f;
       }
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
@@ -480,6 +479,42 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
     half(std::integral_constant<int, 32>{});
   };
   walk_stages<T>(i_begin, i_end, trip);
+  // Rows of inf or NaN in the tiles that were cleaned of them, for the keys that see them: dv takes dout's as they are (a weight is
+  // positive), dk is NaN where q's are (0 * inf: such a score is one of -inf, or capped, or NaN), and delta, made of dout as it is,
+  // has already reached all of dk.  The walk only remembers that there were any.
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(bad[0] | bad[1]) != 0u, 0))
+    for (int i = i_begin; i < i_end; ++i) {
+      const int ln = TIGHT ? lane_anew() : lane, thread = 64 * wave + ln, h = ln >> 5;
+      const int x0 = (t_begin + i % n) * kRows, head_now = kv_head * p.group + i / n;
+      if (covers(gs, x0, kRows)) continue;
+      const unsigned char* qs = p.q + b * p.sq.batch + head_now * p.sq.head + (long long)x0 * p.sq.token;
+      const unsigned char* ds = p.dout + b * p.sdo.batch + head_now * p.sdo.head + (long long)x0 * p.sdo.token;
+      __syncthreads();
+      if (thread < 2) bad[thread] = 0u;
+      __syncthreads();
+      mark_rows<T, D>(qs, p.sq.token, p.q_len - x0, (LDS_PTR(unsigned))&bad[0], thread);
+      mark_rows<T, D>(ds, p.sdo.token, p.q_len - x0, (LDS_PTR(unsigned))&bad[0], thread);
+      __syncthreads();
+#pragma unroll 1
+      for (int r = 0; r < kRows; ++r) {
+        if (!((__builtin_amdgcn_readfirstlane(bad[r >> 5]) >> (r & 31)) & 1u)) continue;
+        const unsigned char *qr = qs + r * p.sq.token + 4 * h * sizeof(T), *dr = ds + r * p.sdo.token + 4 * h * sizeof(T);
+        const Interval rows = seen_s[32 * wave + (ln & 31)];
+        const bool mine = x0 + r >= rows.lo && x0 + r < rows.hi;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            phase<true>();
+            const f32x4 x = four_of<T>(dr + (32 * dt + 2 * e) * sizeof(T)), y = four_of<T>(qr + (32 * dt + 2 * e) * sizeof(T));
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              dv[dt][e + u] += mine && !(fabsf(x[u]) < INFINITY) ? x[u] : 0.f;
+              dk[dt][e + u] = fmaf(mine ? y[u] : 0.f, 0.f, dk[dt][e + u]);
+            }
+          }
+      }
+    }
 
   if (plan.deal.n_parts > 1) {
     const size_t item = ((size_t)bk * plan.deal.n_tiles + kt) * plan.deal.n_parts + share.part;

@@ -473,3 +473,70 @@ def test_more_documents_than_30_bits_count(lib):
     want, got = step(short), step(borders)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def alike(got, want, bound):
+    """Finite where the other is, within the bound; else the same infinity or NaN."""
+    fin = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isfinite(got), fin)
+    assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+    assert np.all(np.abs(got[fin] - want[fin]) <= bound[fin])
+
+
+BORDERS = [(True, None, None), (True, [[0, 70, 90, 170]], None), (False, [[0, 100, 190]], None), (True, None, [[30]])]
+
+
+@pytest.mark.parametrize("mask", BORDERS, ids=str)
+@pytest.mark.parametrize("softcap", [0.0, 4.0])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp32", 128), ("fp32", 64)])
+def test_a_broken_row_of_dout_reaches_the_keys_that_it_sees(lib, dtype, d, softcap, mask):
+    """Infinities and NaN in dout, in tiles that a workgroup's keys see in part and as a whole: dv takes each in its own channel,
+    dk of the keys that such rows see is not finite, and nothing else changes."""
+    causal, docs, prefix = mask
+    n = 200
+    q, k, v, dout = make(51, 1, 4, 2, n, n, d, dtype)
+    clean, rows = dout.clone(), {20: float("nan"), 75: float("-inf"), 100: float("nan"), 101: float("inf"), 150: float("inf")}
+    for i, (row, x) in enumerate(rows.items()):
+        dout[0, i % 4, row, 5 + 9 * i], clean[0, i % 4, row, 5 + 9 * i] = x, 0.0
+    args = dict(causal=causal, doc_offsets=ints(docs), prefix=ints(prefix), softcap=softcap)
+    out, lse = lib.masked_attention(q, k, v, want_lse=True, **args)
+    dq, dk, dv = (f64(x) for x in lib.masked_attention_backward(q, k, v, out, lse, dout, **args))
+    torch.cuda.synchronize()
+    see, scale = mo.visible(1, n, n, causal, docs, prefix), lib.resolved_scale(d)
+    ref = mo.attention(f64(q), f64(k), f64(v), see, scale, softcap, dout=f64(clean))
+    bounds = mo.gradient_bounds(ref, 2.0 ** -7 if dtype == "bf16" else 2.0 ** -23, n_terms(2 * n, d), scale)
+    for i, (row, x) in enumerate(rows.items()):                    # weights are positive: these rows see keys of finite scores
+        head, seen = i % 4, see[0, row]
+        ref["dv"][0, head // 2, seen, 5 + 9 * i] += x
+        ref["dk"][0, head // 2, seen] = np.nan
+        ref["dq"][0, head, row] = np.nan if seen.any() else 0.0
+    alike(dv, ref["dv"], bounds["dv"])
+    for got, name in ((dq, "dq"), (dk, "dk")):                     # inf - inf, or inf: which one is a matter of order
+        alike(np.where(np.isfinite(got), got, np.nan), ref[name], bounds[name])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp32", 128)])
+def test_a_value_of_infinity_leaves_dv_alone(lib, dtype, d):
+    """dv is made of weights and dout; what an infinite value makes of out and delta is not in it.  An infinite query of capped
+    scores (all of them the cap, slope 0) is NaN in its channel of dk."""
+    n = 150
+    q, k, v, dout = make(52, 1, 2, 1, n, n, d, dtype)
+    ref = mo.attention(f64(q), f64(k), f64(v), mo.visible(1, n, n, True), lib.resolved_scale(d), dout=f64(dout))
+    bounds = mo.gradient_bounds(ref, 2.0 ** -7 if dtype == "bf16" else 2.0 ** -23, n_terms(2 * n, d), lib.resolved_scale(d))
+    v[0, 0, 60, 3] = float("inf")
+    out, lse = lib.masked_attention(q, k, v, causal=True, want_lse=True)
+    dv = lib.masked_attention_backward(q, k, v, out, lse, dout, causal=True)[2]
+    torch.cuda.synchronize()
+    alike(f64(dv), ref["dv"], bounds["dv"])
+    q, k, v, dout = make(53, 1, 2, 1, n, n, d, dtype)
+    k += torch.where(k >= 0, 0.25, -0.25).to(k.dtype)               # no score of 0 * inf
+    big = q.clone()
+    q[0, 1, 70, 9], big[0, 1, 70, 9] = float("inf"), 1e30            # the same capped scores
+    got, want = [], []
+    for x, res in ((q, got), (big, want)):
+        out, lse = lib.masked_attention(x, k, v, causal=True, softcap=5.0, want_lse=True)
+        res += [out, lse, *lib.masked_attention_backward(x, k, v, out, lse, dout, causal=True, softcap=5.0)]
+    torch.cuda.synchronize()
+    assert torch.isnan(got[3][0, 0, :71, 9]).all() and torch.isfinite(want[3]).all()
+    got[3][0, 0, :71, 9] = want[3][0, 0, :71, 9]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
