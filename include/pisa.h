@@ -252,7 +252,8 @@ int32_t dense_attention(const pisa_shape* shape, const void* q, const void* k, c
  *                  equal neighbours are an empty document; what lies before the first or behind the last offset is
  *                  padding).  A row sees the keys of its own document; with causal, those up to
  *                  max(pos_i, doc_offsets[b][c] + prefix[b][c] - 1).
- * A row that sees no key has out = 0 and lse = -inf (and gradients of 0; keys no row sees have gradients of 0 as well).
+ * A row that sees no key, or only keys with scores of -inf, has out = 0 and lse = -inf, a dq of 0, and adds nothing to dk and
+ * dv; keys no row sees have gradients of 0 as well.
  * What a row does not see does not reach it, whatever it holds: keys and values of infinity or NaN that are masked for
  * row i, and query rows of infinity or NaN that do not see key j, leave out_i and the gradients of key j as they are.
  * Strides are counted in elements, the channels of a row lie together; every stride has to be a multiple of 16 bytes
@@ -356,7 +357,8 @@ int32_t pisa_paged_append(const pisa_paged_shape* shape, const void* k, const vo
 /*
  * One query row per sequence and head, at position lengths[s] - 1, over all cached tokens of its sequence:
  *   z_j = scale q . k_j, capped and biased by slopes[h] (lengths[s] - 1 - j) as in pisa_masked_attention,
- *   out = sum_j exp(z_j - lse) v_j.  A sequence of length 0 has out = 0 and lse = -inf.
+ *   out = sum_j exp(z_j - lse) v_j.  A sequence of length 0, or of scores of -inf alone, has
+ *   out = 0 and lse = -inf.
  * The cached tokens of all sequences are shared out evenly among the workgroups, whatever their lengths, and the parts of a
  * sequence joined in a fixed order.
  *   q, out     [seqs, heads, d], shape->dtype, dense

@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
   if (t_begin < t_end) load(t_begin, 0);
 
   u32x4 q[G::STEPS], g[G::STEPS];                // the lane's rows of q and dout; zeros where the row sees nothing
-  float delta = 0.f, minus_lse = 0.f;
+  float delta = 0.f, minus_lse = -INFINITY;      // rows without a score above -inf: all weights 0
   {
     const unsigned char* qs = p.q + b * p.sq.batch + head * p.sq.head + (long long)row * p.sq.token;
     const unsigned char* gsrc = p.dout + b * p.sdo.batch + head * p.sdo.head + (long long)row * p.sdo.token;
@@ -181,8 +181,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
       }
     }
     delta += __shfl_xor(delta, 32);
-    if (sees) minus_lse = -in_domain<T>(p.lse[(size_t)bh * p.q_len + row]);
+    const float lse = sees ? p.lse[(size_t)bh * p.q_len + row] : -INFINITY;
+    if (lse != -INFINITY) minus_lse = -in_domain<T>(lse);
   }
+  const bool some = minus_lse != -INFINITY;
   const Scorer<T, MOD> sc(p, head);
   const int pos = row + p.kv_len - p.q_len;
 
@@ -314,15 +316,15 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
   if (row < p.q_len && h == 0 && share.part == 0) {
     float* st = plan.stat + (size_t)bh * p.q_len + row;
     st[0] = minus_lse;
-    st[(size_t)p.batch * p.heads * p.q_len] = sees ? delta : 0.f;
+    st[(size_t)p.batch * p.heads * p.q_len] = some ? delta : 0.f;
   }
   if (!MENDS && plan.deal.n_parts > 1) {
     const size_t item = ((size_t)bh * plan.deal.n_tiles + qt) * plan.deal.n_parts + share.part;
-    store_row<float, D>(reinterpret_cast<unsigned char*>(plan.part + (item * kOwn + 32 * wave + lam) * D), acc, p.scale, sees, h);
+    store_row<float, D>(reinterpret_cast<unsigned char*>(plan.part + (item * kOwn + 32 * wave + lam) * D), acc, p.scale, some, h);
     return;
   }
   if (row < p.q_len)
-    store_row<T, D>(p.dq + b * p.sdq.batch + head * p.sdq.head + (long long)row * p.sdq.token, acc, p.scale, sees, h);
+    store_row<T, D>(p.dq + b * p.sdq.batch + head * p.sdq.head + (long long)row * p.sdq.token, acc, p.scale, some, h);
 }
 
 template <typename T, int D, int MOD>

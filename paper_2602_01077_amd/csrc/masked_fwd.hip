@@ -328,6 +328,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
     return;
   }
   if (row < p.q_len) {
+    const bool some = sees && st.l != 0.f;       // false: no key, or none with a score above -inf
     const float inv = 1.f / st.l;
     unsigned char* dst = p.out + b * p.so.batch + head * p.so.head + (long long)row * p.so.token;
 #pragma unroll
@@ -336,14 +337,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
       for (int g = 0; g < 4; ++g) {
         f32x4 x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = sees ? st.o[dt][4 * g + e] * inv : 0.f;
+        for (int e = 0; e < 4; ++e) x[e] = some ? st.o[dt][4 * g + e] * inv : 0.f;
         const int ch = 32 * dt + 8 * g + 4 * h;
         if constexpr (sizeof(T) == 2)
           *reinterpret_cast<u32x2*>(dst + 2 * ch) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
         else
           *reinterpret_cast<f32x4*>(dst + 4 * ch) = x;
       }
-    if (p.lse && h == 0) p.lse[(size_t)bh * p.q_len + row] = sees ? log_sum<T>(st.m, st.l) : -INFINITY;
+    if (p.lse && h == 0) p.lse[(size_t)bh * p.q_len + row] = some ? log_sum<T>(st.m, st.l) : -INFINITY;
   }
 }
 

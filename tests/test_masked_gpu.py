@@ -540,3 +540,39 @@ def test_a_value_of_infinity_leaves_dv_alone(lib, dtype, d):
     assert torch.isnan(got[3][0, 0, :71, 9]).all() and torch.isfinite(want[3]).all()
     got[3][0, 0, :71, 9] = want[3][0, 0, :71, 9]
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("n,m,docs,heads", [(100, 100, None, 2), (100, 1000, [[0, 920, 1000]], 2), (300, 300, [[0, 20, 300]], 300)], ids=str)
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp32", 128), ("fp32", 64)])
+def test_rows_of_scores_of_minus_infinity_alone(lib, dtype, d, bias, n, m, docs, heads):
+    """Keys masked by a channel of the type's lowest value, whose scores overflow to -inf: rows that see no other key have out 0,
+    lse -inf and no part in the gradients, however their keys are shared out; for the others such keys are not there."""
+    q, k, v, dout = make(54, 1, heads, 1, n, m, d, dtype)
+    last = docs[0][1] if docs else 10                              # the keys before it
+    q[..., 4], k[..., 4] = 2.0, 0.5
+    k[:, :, :last, 4] = torch.finfo(k.dtype).min
+    slopes = torch.linspace(0.0, 0.5, heads, device=DEV) if bias else None
+    args = dict(causal=docs is None, doc_offsets=ints(docs), slopes=slopes)
+    out, lse = lib.masked_attention(q, k, v, want_lse=True, **args)
+    grads = lib.masked_attention_backward(q, k, v, out, lse, dout, **args)
+    torch.cuda.synchronize()
+    see = mo.visible(1, n, m, docs is None, docs)
+    see[:, :, :last] = False
+    empty = ~see[0].any(1)
+    assert empty.any() and not empty.all()
+    assert torch.isneginf(lse[:, :, empty]).all() and torch.count_nonzero(out[:, :, empty]) == 0
+    pick = slice(0, 2) if heads > 2 else slice(None)               # of many heads, out and dq of two are compared
+    scale, slo = lib.resolved_scale(d), None if slopes is None else slopes.double().cpu().numpy()[pick]
+    ref = mo.attention(f64(q)[:, pick], f64(k), f64(v), see, scale, 0.0, slo, f64(dout)[:, pick])
+    eps = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -23
+    assert np.all(np.abs(f64(out)[:, pick] - ref["out"]) <= mo.forward_bounds(ref, eps, n_terms(m, d)))
+    bounds = mo.gradient_bounds(ref, eps, n_terms(max(m, 2 * n), d), scale)
+    for name, got in zip(("dq", "dk", "dv"), grads):
+        got = f64(got)
+        if name == "dq":
+            assert np.all(got[:, :, empty] == 0) and np.all(np.abs(got[:, pick] - ref[name]) <= bounds[name])
+        elif heads == 2:
+            assert np.all(np.abs(got - ref[name]) <= bounds[name]), name
+        else:
+            assert np.isfinite(got).all() and np.all(got[:, :, :last] == 0)

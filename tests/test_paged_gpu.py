@@ -317,3 +317,18 @@ def test_two_calls_at_once(lib):
                 got.append(lib.paged_attention(*c, want_lse=True))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_scores_of_minus_infinity_alone(lib, dtype):
+    """A cached sequence whose keys all score -inf has out 0 and lse -inf, in one workgroup as over many."""
+    for lengths in ([40, 100], [3000, 700]):
+        kp, vp, table, rows = cache(26, lengths, 2, 16, 64, dtype)
+        q = torch.randn(2, 4, 64, generator=torch.Generator().manual_seed(27)).to(DT[dtype]).to(DEV)
+        q[..., 7] = 2.0
+        kp[table[0, :-(-lengths[0] // 16)].long(), :, :, 7] = torch.finfo(kp.dtype).min
+        out, lse = lib.paged_attention(q, kp, vp, table, torch.tensor(lengths, dtype=torch.int32, device=DEV), want_lse=True)
+        torch.cuda.synchronize()
+        assert torch.count_nonzero(out[0]) == 0 and torch.isneginf(lse[0]).all()
+        ref = oracle(q, rows, [0, lengths[1]], lib.resolved_scale(64))
+        close(out, lse, ref, dtype, lengths[1], 64)
