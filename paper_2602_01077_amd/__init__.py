@@ -391,8 +391,13 @@ def _masked_call(q, k, v, out, causal, doc_offsets, softcap, scale):
 
 def masked_attention_workspace_bytes(q, k, v, causal: bool = False, doc_offsets: Optional[torch.Tensor] = None,
                                      backward: bool = False) -> int:
-    """Bytes of workspace that masked_attention, or masked_attention_backward, needs for tensors of these shapes."""
-    return _masked_call(q, k, v, q, causal, doc_offsets, 0.0, None)[2 if backward else 1]
+    """Bytes of workspace that masked_attention, or masked_attention_backward, needs for tensors of these shapes.  Raises what
+    those would for shapes that they refuse."""
+    out = torch.empty_like(q, device="meta")     # laid out as masked_attention lays out its own (q may be expanded, out never is)
+    shape, forward, back = _masked_call(q, k, v, out, causal, doc_offsets, 0.0, None)
+    if not back:                                 # a shape that is taken has some
+        _check(_lib.pisa_masked_attention(shape, *[None] * 9, 0, None))
+    return back if backward else forward
 
 
 def masked_attention(q, k, v, causal: bool = False, doc_offsets: Optional[torch.Tensor] = None,
@@ -487,8 +492,12 @@ def paged_append(k, v, offsets, k_pages, v_pages, page_table, lengths) -> None:
 
 
 def paged_attention_workspace_bytes(q, k_pages, v_pages, page_table) -> int:
-    """Bytes of workspace that paged_attention needs for tensors of these shapes (whatever the lengths)."""
-    return _paged_call(k_pages, v_pages, page_table, q.shape[1], 0.0, None)[1]
+    """Bytes of workspace that paged_attention needs for tensors of these shapes (whatever the lengths).  Raises what that would
+    for shapes that it refuses."""
+    shape, need = _paged_call(k_pages, v_pages, page_table, q.shape[1], 0.0, None)
+    if not need:
+        _check(_lib.pisa_paged_attention(shape, *[None] * 9, 0, None))
+    return need
 
 
 def paged_attention(q, k_pages, v_pages, page_table, lengths, softcap: float = 0.0, slopes: Optional[torch.Tensor] = None,

@@ -211,3 +211,35 @@ def test_one_slot_for_a_whole_page_is_refused():
             pisa.paged_attention(torch.zeros(2, 4, 64), k, v, table, lengths)
         with pytest.raises(ValueError, match=f"{name}: one row"):
             pisa.paged_append(torch.zeros(3, 2, 64), torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int32), k, v, table, lengths)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_workspaces_of_expanded_tensors(dtype):
+    """A tensor that stands for all batch elements and heads needs the workspace of a dense one, in either memory order."""
+    one = lambda n: torch.zeros(1, 1, n, 128, dtype=dtype)
+    for b, h, n, m in ((2, 4, 3, 9000), (2, 4, 1, 700), (1, 24, 700, 700)):
+        q, k, v = (one(x).expand(b, h, x, 128) for x in (n, m, m))
+        for backward in (False, True):
+            want = pisa.masked_attention_workspace_bytes(*(x.contiguous() for x in (q, k, v)), causal=True, backward=backward)
+            assert pisa.masked_attention_workspace_bytes(q, k, v, causal=True, backward=backward) == want
+        assert want > 0
+        first = lambda x: x.transpose(1, 2).contiguous().transpose(1, 2)
+        assert pisa.masked_attention_workspace_bytes(first(q), k, v, causal=True, backward=True) == want
+
+
+def test_workspaces_of_refused_shapes_raise():
+    q = torch.zeros(1, 5, 8, 64)
+    with pytest.raises(pisa.PisaError, match="kv_heads") as e:
+        pisa.masked_attention_workspace_bytes(q, q[:, :2], q[:, :2])
+    assert e.value.code == BAD
+    with pytest.raises(pisa.PisaError) as e:
+        pisa.masked_attention_workspace_bytes(torch.zeros(1, 1, 8, 96), torch.zeros(1, 1, 8, 96), torch.zeros(1, 1, 8, 96))
+    assert e.value.code == BAD
+    wide = torch.zeros(1, 1, 1, 64).expand(70000, 1, 1, 64)
+    with pytest.raises(pisa.PisaError, match="65535") as e:
+        pisa.masked_attention_workspace_bytes(wide, wide, wide)
+    assert e.value.code == NOT_BUILT
+    pages, table = torch.zeros(4, 16, 2, 64), torch.zeros(2, 3, dtype=torch.int32)
+    with pytest.raises(pisa.PisaError, match="kv_heads"):
+        pisa.paged_attention_workspace_bytes(torch.zeros(2, 5, 64), pages, pages, table)
+    assert pisa.paged_attention_workspace_bytes(torch.zeros(2, 4, 64), pages, pages, table) > 0
