@@ -256,6 +256,7 @@ int32_t dense_attention(const pisa_shape* shape, const void* q, const void* k, c
  * dv; keys no row sees have gradients of 0 as well.
  * What a row does not see does not reach it, whatever it holds: keys and values of infinity or NaN that are masked for
  * row i, and query rows of infinity or NaN that do not see key j, leave out_i and the gradients of key j as they are.
+ * Weighted values are summed before they are divided by the weights' sum: magnitudes in v up to 2^102 cannot overflow there.
  * Strides are counted in elements, the channels of a row lie together; every stride has to be a multiple of 16 bytes
  * and no negative number, a token stride below 2^31 / 64 bytes.  Batch or head strides of 0 are allowed for inputs
  * (one tensor for all), not for outputs of more than one batch element or head.  All strides 0: dense
@@ -358,7 +359,7 @@ int32_t pisa_paged_append(const pisa_paged_shape* shape, const void* k, const vo
  * One query row per sequence and head, at position lengths[s] - 1, over all cached tokens of its sequence:
  *   z_j = scale q . k_j, capped and biased by slopes[h] (lengths[s] - 1 - j) as in pisa_masked_attention,
  *   out = sum_j exp(z_j - lse) v_j.  A sequence of length 0, or of scores of -inf alone, has
- *   out = 0 and lse = -inf.
+ *   out = 0 and lse = -inf.  Magnitudes in v up to 2^97 cannot overflow in the sums.
  * The cached tokens of all sequences are shared out evenly among the workgroups, whatever their lengths, and the parts of a
  * sequence joined in a fixed order.
  *   q, out     [seqs, heads, d], shape->dtype, dense

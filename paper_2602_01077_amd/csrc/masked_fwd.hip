@@ -96,9 +96,9 @@ __device__ __forceinline__ float weigh(const Score<T, MOD>& sc, const f32x16& s,
   return a + b;
 }
 
-// The maximum is taken anew only where a sum of weights against the old one nears overflow (and on a wave's first tile, whose
-// old maximum is -inf): fp32 and bf16 share their exponents, so a stale maximum costs no digits.  What it costs is range: values
-// have to stay this factor below the largest number.
+// The maximum is taken anew only where a lane's sum of weights against the old one reaches this (and on a wave's first tile, whose
+// old maximum is -inf): fp32 and bf16 share their exponents, so a stale maximum costs no digits.  What it costs is range: weighted
+// values are summed up to twice this factor (a row has two lanes), so values of 2^102 and less are safe whatever the scores.
 constexpr float kStaleLimit = 0x1p24f;
 
 template <typename T, int D, int MOD>
@@ -257,10 +257,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
           sum += weigh<T, MOD, false>(sc, s1, sc.c, sc.slope, -st.m, ahead - 32.f, w1, top);
         }
       }
-      if (__builtin_expect(__any(!(sum < kStaleLimit)), 0)) {
+      if (__builtin_expect(__any(!(st.l + sum < kStaleLimit)), 0)) {
         // Row by row, so that what a row gives does not hang on its neighbours.  The scores are rounded as the maximum is taken
-        // of them: the largest key has weight 1, whatever its size.
-        bool again = !(sum < kStaleLimit);
+        // of them: the largest key has weight 1, whatever its size.  Where the sum was made by earlier tiles, it is what the
+        // maximum is raised by.
+        bool again = !(st.l + sum < kStaleLimit);
         again |= (bool)__shfl_xor((int)again, 32);
         if (near) {
           cap_scores<T>(s0, sc.to_cap, sc.cap);
@@ -281,7 +282,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
             }
           }
         }
-        raise_max<T, D>(st, again ? fmaxf(max_of(s0), max_of(s1)) : -INFINITY);
+        raise_max<T, D>(st, again ? fmaxf(fmaxf(max_of(s0), max_of(s1)), st.m + log_of<T>(st.l)) : -INFINITY);
         const float nm = st.m == -INFINITY ? 0.f : -st.m;
         sum = weigh<T, MOD, false>(sc, s0, c2, slope2, nm, ahead, w0, top);
         sum += weigh<T, MOD, false>(sc, s1, c2, slope2, nm, ahead - 32.f, w1, top);
@@ -371,7 +372,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void masked_join_
     float top = m;
 #pragma unroll
     for (int u = 0; u < 8; ++u)
-      if (i0 + u < n_parts) top = fmaxf(top, mi[u]);
+      if (i0 + u < n_parts) top = fmaxf(top, mi[u] + log_of<T>(li[u]));      // a maximum can be stale by as much as its sum has grown
     if (l != 0.f) {
       const float f = exp_of<T>(m - top);
       l *= f;

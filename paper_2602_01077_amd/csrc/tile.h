@@ -264,9 +264,10 @@ template <typename T> __device__ __forceinline__ float exp_diff(float s, float c
   return __builtin_amdgcn_exp2f(fmaf(s, c, minus_m) * kLog2e);
 }
 template <typename T> __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(sizeof(T) == 2 ? x : x * kLog2e); }
+template <typename T> __device__ __forceinline__ float log_of(float x) { return sizeof(T) == 2 ? __builtin_amdgcn_logf(x) : logf(x); }
 // log of a sum of weights in that domain, and its way to the natural one
 template <typename T> __device__ __forceinline__ float log_sum(float m, float l) {
-  return sizeof(T) == 2 ? (m + __builtin_amdgcn_logf(l)) * kLn2 : m + logf(l);
+  return sizeof(T) == 2 ? (m + log_of<T>(l)) * kLn2 : m + log_of<T>(l);
 }
 
 __device__ __forceinline__ float max_of(const f32x16& s) {

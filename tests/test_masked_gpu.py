@@ -576,3 +576,26 @@ def test_rows_of_scores_of_minus_infinity_alone(lib, dtype, d, bias, n, m, docs,
             assert np.all(np.abs(got - ref[name]) <= bounds[name]), name
         else:
             assert np.isfinite(got).all() and np.all(got[:, :, :last] == 0)
+
+
+@pytest.mark.parametrize("heads,n,m", [(8, 1024, 20000), (1, 1, 20000), (64, 1024, 5000)], ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_large_values_under_scores_that_rise(lib, dtype, heads, n, m):
+    """Values near 2^102 under scores that pass the first tile's maximum by as much as it may be stale, in every later tile or for a
+    while: sums of weighted values stay in range, in one walk as in parts."""
+    g = torch.Generator().manual_seed(55)
+    k = torch.zeros(1, 1, m, 64)
+    v = (2.0 ** 101 * (1 + torch.rand(1, 1, m, 64, generator=g))).to(DT[dtype])
+    q = torch.zeros(1, heads, n, 64)
+    q[..., 0] = 1.0
+    for rise in (slice(64, None), slice(64, 2000), slice(1000, None, 3)):
+        k.zero_()
+        k[0, 0, rise, 0] = 104.5                                   # 2^18.8 times the first keys' weight, 32 keys to a lane and tile
+        qd, kd, vd = (x.to(DT[dtype]).to(DEV) for x in (q, k, v))
+        out, lse = lib.masked_attention(qd, kd, vd, want_lse=True)
+        torch.cuda.synchronize()
+        ref = mo.attention(f64(qd)[:, :1, :1], f64(kd), f64(vd), np.ones((1, 1, m), bool), lib.resolved_scale(64))
+        eps = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -23
+        bound = mo.forward_bounds(ref, eps, n_terms(m, 64))
+        assert np.all(np.abs(f64(out) - ref["out"]) <= bound)
+        assert np.abs(f64(lse) - ref["lse"]).max() <= 2.0 ** -24 * n_terms(m, 64) * (1 + ref["zmax"])
