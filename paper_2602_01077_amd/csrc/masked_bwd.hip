@@ -485,8 +485,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
   // positive), dk is NaN where q's are (0 * inf: such a score is one of -inf, or capped, or NaN), and delta, made of dout as it is,
   // has already reached all of dk.  The walk only remembers that there were any.
   if (__builtin_expect(__builtin_amdgcn_readfirstlane(bad[0] | bad[1]) != 0u, 0))
-    for (int i = i_begin; i < i_end; ++i) {
-      const int ln = TIGHT ? lane_anew() : lane, thread = 64 * wave + ln, h = ln >> 5;
+    for (int i = 0; i < n * p.group; ++i) {      // all steps, those of other parts as well: either way the sums are not finite
+      const int ln = lane_anew(), thread = 64 * wave + ln, h = ln >> 5;
       const int x0 = (t_begin + i % n) * kRows, head_now = kv_head * p.group + i / n;
       if (covers(gs, x0, kRows)) continue;
       const unsigned char* qs = p.q + b * p.sq.batch + head_now * p.sq.head + (long long)x0 * p.sq.token;
