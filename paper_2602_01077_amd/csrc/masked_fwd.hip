@@ -229,15 +229,18 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
     if (touches(ws, t * kRows, kRows)) {
       const float ahead = MOD & BIAS ? (float)(pos - t * kRows - 4 * h) : 0.f;
       const bool whole = covers(ws, t * kRows, kRows);
-      bool near = sizeof(T) == 2 && (MOD & CAP) && whole && sc.direct && i > 0;
+      const bool near = sizeof(T) == 2 && (MOD & CAP) && whole && sc.direct && i > 0;
+      bool far = true;                           // this lane's scores are to be capped as they stand
       Weights<T> w0, w1;
       float sum = INFINITY, top = 0.f;           // the first tile has no maximum to be weighed against
       if (near) {
         sum = weigh<T, MOD, true>(sc, s0, 1.f, sc.slope, -st.m, ahead, w0, top);
         sum += weigh<T, MOD, true>(sc, s1, 1.f, sc.slope, -st.m, ahead - 32.f, w1, top);
-        near = !__any(!(top <= sc.near_limit));
+        far = !(top <= sc.near_limit);
       }
-      if (!near) {
+      // Lane by lane, so that what a row gives does not hang on what its neighbours hold.  (The hint keeps this out of the way of
+      // capped tiles: 24 heads of 4 608 tokens, capped and biased, 350 us without it, 324 with.)
+      if (__builtin_expect(far, 0)) {
         if (MOD & CAP) {
           cap_scores<T>(s0, sc.to_cap, sc.cap);
           cap_scores<T>(s1, sc.to_cap, sc.cap);
@@ -258,34 +261,37 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
         }
       }
       if (__builtin_expect(__any(!(st.l + sum < kStaleLimit)), 0)) {
-        // Row by row, so that what a row gives does not hang on its neighbours.  The scores are rounded as the maximum is taken
-        // of them: the largest key has weight 1, whatever its size.  Where the sum was made by earlier tiles, it is what the
-        // maximum is raised by.
+        // Row by row.  The scores are rounded as the maximum is taken of them: the largest key has weight 1, whatever its
+        // size.  Where the sum was made by earlier tiles, it is what the maximum is raised by.
         bool again = !(st.l + sum < kStaleLimit);
         again |= (bool)__shfl_xor((int)again, 32);
-        if (near) {
-          cap_scores<T>(s0, sc.to_cap, sc.cap);
-          cap_scores<T>(s1, sc.to_cap, sc.cap);
-        }
-        const float f = again ? sc.c : 1.f, c2 = again ? 1.f : sc.c;
-        const float slope1 = again ? sc.slope : 0.f, slope2 = again ? 0.f : sc.slope;
-        {
+        float peak = -INFINITY;
+        if (again) {
+          if (!far) {
+            cap_scores<T>(s0, sc.to_cap, sc.cap);
+            cap_scores<T>(s1, sc.to_cap, sc.cap);
+          }
+          {
 #pragma clang fp contract(off)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float key = (float)((r / 4) * 8 + r % 4);
-            s0[r] *= f;
-            s1[r] *= f;
-            if (MOD & BIAS) {
-              s0[r] -= slope1 * fabsf(ahead - key);
-              s1[r] -= slope1 * fabsf(ahead - 32.f - key);
+            for (int r = 0; r < 16; ++r) {
+              const float key = (float)((r / 4) * 8 + r % 4);
+              s0[r] *= sc.c;
+              s1[r] *= sc.c;
+              if (MOD & BIAS) {
+                s0[r] -= sc.slope * fabsf(ahead - key);
+                s1[r] -= sc.slope * fabsf(ahead - 32.f - key);
+              }
             }
           }
+          peak = fmaxf(fmaxf(max_of(s0), max_of(s1)), st.m + log_of<T>(st.l));
         }
-        raise_max<T, D>(st, again ? fmaxf(fmaxf(max_of(s0), max_of(s1)), st.m + log_of<T>(st.l)) : -INFINITY);
-        const float nm = st.m == -INFINITY ? 0.f : -st.m;
-        sum = weigh<T, MOD, false>(sc, s0, c2, slope2, nm, ahead, w0, top);
-        sum += weigh<T, MOD, false>(sc, s1, c2, slope2, nm, ahead - 32.f, w1, top);
+        raise_max<T, D>(st, peak);
+        if (again) {
+          const float nm = st.m == -INFINITY ? 0.f : -st.m;
+          sum = weigh<T, MOD, false>(sc, s0, 1.f, 0.f, nm, ahead, w0, top);
+          sum += weigh<T, MOD, false>(sc, s1, 1.f, 0.f, nm, ahead - 32.f, w1, top);
+        }
       }
       st.l += sum;
       cols_times<T, D, 0>(rd, v_off, w0, st.o);

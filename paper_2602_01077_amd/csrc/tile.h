@@ -301,7 +301,7 @@ struct Near {                                    // mult tanh(x) = x of(x^2)
 template <typename T> __device__ __forceinline__ float tanh_times(float x, const Near& near, float mult) {
   if (sizeof(T) == 4) return mult * tanhf(x);
   const float far = fmaf(-2.f * mult, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.f * kLog2e)) + 1.f), mult);
-  return fabsf(x) <= kNear ? x * near.of(x * x) : far;
+  return x * x <= kNear * kNear ? x * near.of(x * x) : far;          // the line that cap_scores draws
 }
 // s = mult tanh(to_cap s), to_cap > 0, for 32 rows' worth of scores.
 template <typename T> __device__ __forceinline__ void cap_scores(f32x16& s, float to_cap, float mult) {

@@ -599,3 +599,29 @@ def test_large_values_under_scores_that_rise(lib, dtype, heads, n, m):
         bound = mo.forward_bounds(ref, eps, n_terms(m, 64))
         assert np.all(np.abs(f64(out) - ref["out"]) <= bound)
         assert np.abs(f64(lse) - ref["lse"]).max() <= 2.0 ** -24 * n_terms(m, 64) * (1 + ref["zmax"])
+
+
+@pytest.mark.parametrize("softcap,bias", [(0.0, False), (0.0, True), (30.0, False), (6.0, False), (30.0, True)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp32", 64)])
+def test_a_row_does_not_hang_on_what_its_neighbours_hold(lib, dtype, d, softcap, bias):
+    """Queries of NaN, of infinity, and fifty times as long: the other rows' results keep their bits, and so do the gradients of the
+    keys that only others see."""
+    n, m = 200, 700
+    q, k, v, dout = make(56, 1, 2, 1, n, m, d, dtype)
+    args = dict(causal=True, softcap=softcap, slopes=torch.tensor([0.05, 0.01], device=DEV) if bias else None)
+
+    def step(x):
+        out, lse = lib.masked_attention(x, k, v, want_lse=True, **args)
+        return (out, lse, *lib.masked_attention_backward(x, k, v, out, lse, dout, **args))
+    want = step(q)
+    for row in (0, 45, 130):
+        for change in (lambda x: float("nan"), lambda x: float("inf"), lambda x: 50 * x):
+            broken = q.clone()
+            broken[:, :, row] = change(q[:, :, row])
+            got = step(broken)
+            torch.cuda.synchronize()
+            rows, first = [i for i in range(n) if i != row], row + m - n + 1
+            for a, b in zip(got[:3], want[:3]):
+                assert torch.equal(a[:, :, rows], b[:, :, rows])
+            for a, b in zip(got[3:], want[3:]):
+                assert torch.equal(a[:, :, first:], b[:, :, first:])
