@@ -256,6 +256,8 @@ int32_t dense_attention(const pisa_shape* shape, const void* q, const void* k, c
  * dv; keys no row sees have gradients of 0 as well.
  * What a row does not see does not reach it, whatever it holds: keys and values of infinity or NaN that are masked for
  * row i, and query rows of infinity or NaN that do not see key j, leave out_i and the gradients of key j as they are.
+ * What it does see acts as the formula says it; where a weight underflows to 0, an infinity that it multiplies can come out
+ * as an infinity or as NaN.
  * Weighted values are summed before they are divided by the weights' sum: magnitudes in v up to 2^102 cannot overflow there.
  * Strides are counted in elements, the channels of a row lie together; every stride has to be a multiple of 16 bytes
  * and no negative number, a token stride below 2^31 / 64 bytes.  Batch or head strides of 0 are allowed for inputs
@@ -306,7 +308,11 @@ int32_t pisa_masked_attention(const pisa_masked_shape* shape, const void* q, con
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i,
  * the last two over the rows that see key j of all query heads that share its head.  slopes are constants here.  Sums are
  * made in a fixed order: equal calls give equal bits.
- *   out, lse  as pisa_masked_attention wrote them for the same arguments
+ *   out, lse  as pisa_masked_attention wrote them for the same arguments.  In PISA_BF16 what out's rounding does to delta is
+ *             mended from dz_i, whose sum over all of the row's keys is 0: out and lse that were joined over several calls, each
+ *             with a part of the keys, give wrong dq and dk for such a part (not so in PISA_FP32, where nothing is mended).
+ *             Weights are as exact as lse is in 32 bits, 2^-23 |lse|: beside a bf16's rounding that is nothing up to |lse| =
+ *             2^12, and with scores of 2^23 and more nothing is left of them.
  *   strides   of dout, dq, dk, dv; NULL: those of out, q, k, v
  *   dq, dk, dv  written, never read; in shape->dtype, sums in fp32, rounded once
  *   workspace pisa_masked_attention_backward_workspace_bytes(shape) bytes, 16-byte aligned
@@ -346,7 +352,8 @@ typedef struct pisa_paged_shape {
  * Writes new tokens into the cache: rows offsets[s] .. offsets[s+1]-1 of k and v become the last tokens of sequence s,
  * positions lengths[s] - (offsets[s+1] - offsets[s]) .. lengths[s] - 1; lengths already count them.  Rows outside
  * [offsets[0], offsets[seqs]) and positions below 0 or past the table are not written anywhere.  Nothing else in the cache
- * is touched.  Two rows for one slot (sequences that share a page) leave either.
+ * is touched.  Two rows for one slot (sequences that share a page) leave it with either, 16 bytes by
+ * 16 bytes.
  *   k, v       [tokens, kv_heads, d], shape->dtype, dense;  tokens >= 0, tokens * kv_heads * d < 2^32
  *   offsets    int32 [seqs + 1], ascending, on the device
  *   page_table int32 [seqs, max_pages], lengths int32 [seqs], on the device

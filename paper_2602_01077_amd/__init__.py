@@ -408,7 +408,8 @@ def masked_attention(q, k, v, causal: bool = False, doc_offsets: Optional[torch.
     """pisa_masked_attention.  q [batch, heads, q_len, d], k and v [batch, kv_heads, kv_len, d], any strides with whole
     rows of channels (a [batch, tokens, heads, d] tensor goes in as its transpose(1, 2)); doc_offsets int32
     [batch, documents + 1], prefix int32 [batch, documents] (or [batch, 1]), slopes fp32 [heads].  Returns (out, lse or None);
-    `out` is laid out as q unless given."""
+    `out` is laid out as q unless given.  Autograd does not see the call: what it returns has no graph, whatever q, k and v
+    require, and gradients are masked_attention_backward's."""
     if out is None:
         out = torch.empty_like(q)
     shape, need, _ = _masked_call(q, k, v, out, causal, doc_offsets, softcap, scale)
@@ -431,7 +432,8 @@ def masked_attention_backward(q, k, v, out, lse, dout, causal: bool = False, doc
                               dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
                               dv: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """pisa_masked_attention_backward: gradients of masked_attention(...) with the same arguments, from its out and lse and
-    the gradient dout of out.  Returns (dq, dk, dv)."""
+    the gradient dout of out.  Returns (dq, dk, dv).  out and lse have to be of these very keys (bf16 counts on it: not of calls
+    over parts of them, joined)."""
     dq = torch.empty_like(q) if dq is None else dq
     dk = torch.empty_like(k) if dk is None else dk
     dv = torch.empty_like(v) if dv is None else dv

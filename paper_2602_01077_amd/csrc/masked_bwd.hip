@@ -8,9 +8,10 @@
 // so that P and dS leave the first products in the lanes in which the second ones take them.  The dk, dv walk goes over the
 // rows of all query heads that share the key head.
 //
-// Bound as the forward pass is, by operands from LDS and the plain operations between the products: 12 heads of 8 192, causal,
-// dq 340 us, dk and dv 407 (matrix cores 60 and 56 % busy); 24 heads of 4 608 without a mask 890 us together, 1 025 TFLOP/s over
-// the seven products.  At 64 channels with capped and biased scores, 2 x 12 heads of 2 777, 112 and 96 us (20 and 27 %).
+// Bound as the forward pass is, by products and plain operations that wait for each other: 12 heads of 8 192, causal, dq 345 us,
+// dk and dv 412 (matrix cores 60 and 56 % busy, LDS 30 and 36 %); 24 heads of 4 608 without a mask 880-920 us together by card,
+// 1 000-1 040 TFLOP/s over the seven products.  At 64 channels with capped and biased scores, 2 x 12 heads of 2 777, 103 and 97 us
+// (matrix cores 20 and 27 %: vector instructions).
 #include <algorithm>
 
 #include "masked.h"
@@ -194,7 +195,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
   // bf16: delta from a rounded out is off by e = -sum_j dz_ij (the sum is 0 otherwise), and dq by -e sum_j p_ij k_j, which is
   // as much as the other roundings together where few keys have most of a row's weight.  e is known when the walk is done; the
   // part of that sum that weights of kHeavy and more have, of which a row has few, is taken out then.  (The others' does not
-  // matter: the sum falls with the number of keys that share the weight, and so does e.)
+  // matter: the sum falls with the number of keys that share the weight, and so does e.)  The two sums a score and the search for
+  // such weights cost 1 % of the backward pass of long calls (24 heads of 4 608 913 -> 921 us; 64 channels 520 -> 540), 17 % of
+  // short ones (8 heads of 1 024 62.8 -> 73.7; 69.6 with weights from 0.1875 on).
   float off = 0.f;
   int n_heavy = 0;
 

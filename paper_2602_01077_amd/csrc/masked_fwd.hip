@@ -7,11 +7,11 @@
 // O^T += V(t)^T P(t)^T and S^T(t+1).  The walk goes over the tiles that some row of the workgroup sees; a wave leaves out
 // those that none of its rows sees, and compares key numbers only in those that some of them see in part.
 //
-// Bound (bf16, 128 channels) by operands from LDS, 1 KB to a matrix instruction, which is the LDS rate itself, and by the softmax
-// beside it: 24 heads of 4 608 tokens without a mask 255 us, 1 020 TFLOP/s; causal, 12 of 8 192, 222 us, matrix cores 58 % busy.
-// 32 rows a wave leave room for two waves on a SIMD, of which one is in its softmax while the other multiplies.  64 channels with
-// capped and biased scores are bound by vector instructions (2 x 12 heads of 2 777 70 us), fp32 by its matrix instruction (8 heads
-// of 4 500, causal, 417 us, 72 % busy).
+// Bound (bf16, 128 channels) by the turns that products, softmax and barriers take: no unit is full.  Causal, 12 heads of 8 192,
+// 225 us: matrix cores 59 % busy, LDS 30 % (each matrix instruction takes a 1 KB operand from there); 24 heads of 4 608 tokens
+// without a mask 250-263 us by card, 1 000-1 040 TFLOP/s.  32 rows a wave leave room for two waves on a SIMD, of which one is in its softmax while
+// the other multiplies.  64 channels with capped and biased scores are bound by vector instructions (2 x 12 heads of 2 777, 70 us:
+// matrix cores 18 %), fp32 by its matrix instruction (8 heads of 4 500, causal, 420 us, 72 % busy).
 #include <algorithm>
 
 #include "masked.h"

@@ -1,16 +1,18 @@
 // Attention of one new token per sequence over a paged cache, and the append that fills it.
 //
-// Bound by reading the cache once, so the work is cut by cached tokens, whatever sequence they belong to: the tiles of all
-// (sequence, key head) units, laid one behind the other, are shared out evenly among a fixed number of workgroups, which
-// find their range from the lengths on the device.  A workgroup walks its range unit by unit; units that it has not to
-// itself leave (maximum, sum, weighted values) in the workspace, and a second launch joins them.
+// Bound by reading the cache (once for every 16 query heads that share a key head), so the work is cut by cached tokens,
+// whatever sequence they belong to: the tiles of all (sequence, key head) units, laid one behind the other, are shared out
+// evenly among a fixed number of workgroups, which find their range from the lengths on the device.  A workgroup walks its
+// range unit by unit; units that it has not to itself leave (maximum, sum, weighted values) in the workspace, and a second
+// launch joins them.
 //
 // A wave takes KT keys of a tile: K and V rows go to its own part of LDS by DMA, two stages, and it waits for its own loads
 // alone (no barriers in the walk).  With v_mfma_f32_16x16x32_bf16 (fp32: 16x16x4) 16 query heads that share the key head are
 // the columns of S^T = K Q^T and O^T = V^T P^T; register r of lane (j, g) holds key 4 g + r and column j, and that order of
 // the keys serves the second product as it stands.
 //
-// Measured: 48 sequences of up to 8 000 tokens, 32 / 8 heads, 167 us (5.1 TB/s); 2 of 200 000, 40 / 8 heads, 255 us (6.0 TB/s).
+// Measured: 2 sequences of 200 000 tokens, 40 / 8 heads, 255 us (6.0 TB/s); 48 of up to 8 000, 32 / 8 heads, 164 us (5.2 TB/s: here a
+// workgroup walks two or three units and fills its pipeline anew for each).
 #include "paged.h"
 #include "tile.h"
 
