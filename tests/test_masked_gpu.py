@@ -625,3 +625,72 @@ def test_a_row_does_not_hang_on_what_its_neighbours_hold(lib, dtype, d, softcap,
                 assert torch.equal(a[:, :, rows], b[:, :, rows])
             for a, b in zip(got[3:], want[3:]):
                 assert torch.equal(a[:, :, first:], b[:, :, first:])
+
+
+def seen_product(p, x, see):
+    """p [i, j] x [j, c] over the seen pairs alone, where x may hold infinities and NaN (p is 0 where nothing is seen)."""
+    r = p @ np.where(np.isfinite(x), x, 0.0)
+    for j, c in zip(*np.nonzero(~np.isfinite(x))):
+        r[:, c] = np.where(see[:, j], r[:, c] + p[:, j] * x[j, c], r[:, c])
+    return r
+
+
+def by_formula(q, k, v, g, see, scale, softcap, slopes):
+    """out, lse, dq, dk, dv of one batch element, heads by heads, with inf and NaN as 64-bit arithmetic has them."""
+    (h, n, d), (kvh, m) = q.shape, k.shape[:2]
+    far = np.abs(np.arange(n)[:, None] + m - n - np.arange(m)[None, :])
+    res = {"out": np.zeros_like(q), "lse": np.full((h, n), -np.inf), "dq": np.zeros_like(q), "dk": np.zeros_like(k), "dv": np.zeros_like(v)}
+    for j in range(h):
+        e = j // (h // kvh)
+        s = (q[j][:, None] * k[e][None]).sum(-1) * scale
+        t = np.tanh(s / softcap) if softcap else s
+        z = (softcap * t if softcap else s) - (slopes[j] * far if slopes is not None else 0.0)
+        z = np.where(see, z, -np.inf)
+        top = z.max(1, keepdims=True) if m else np.full((n, 1), -np.inf)
+        w = np.where(see, np.exp(z - np.where(np.isneginf(top), 0.0, top)), 0.0)
+        total = w.sum(1, keepdims=True)
+        some = total[:, 0] != 0                                    # rows with a score above -inf (or NaN)
+        pair = see & some[:, None]
+        p = np.where(pair, w / np.where(total == 0, 1.0, total), 0.0)
+        res["lse"][j, some] = (top + np.log(total))[some, 0]
+        res["out"][j, some] = seen_product(p, v[e], pair)[some]
+        dp = (g[j][:, None] * v[e][None]).sum(-1)
+        dz = p * (dp - (g[j] * res["out"][j]).sum(1, keepdims=True)) * (1 - t * t if softcap else 1.0)
+        dz = np.where(pair, dz, 0.0)
+        res["dq"][j, some] = scale * seen_product(dz, k[e], pair)[some]
+        res["dk"][e] += scale * seen_product(dz.T, q[j], pair.T)
+        res["dv"][e] += seen_product(p.T, g[j], pair.T)
+    return res
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("fp32", 128), ("fp32", 64)])
+@pytest.mark.parametrize("seed", range(8))
+def test_drawn_calls_with_broken_elements(lib, seed, dtype, d):
+    """An infinity or NaN somewhere in q, k, v or dout: what is finite by the formula is so and has its value, and what is not
+    finite by the formula is not finite."""
+    rng = np.random.default_rng([seed, d, dtype == "fp32", 1])
+    kvh, group, n = int(rng.integers(1, 3)), int(rng.integers(1, 3)), int(rng.integers(2, 200))
+    m = n if rng.random() < 0.5 else int(rng.integers(2, 300))
+    causal = bool(rng.random() < 0.6)
+    docs = [sorted(int(x) for x in rng.integers(0, m + 1, int(rng.integers(2, 6))))] if rng.random() < 0.6 else None
+    prefix = [[int(x) for x in rng.integers(0, m + 9, len(docs[0]) - 1 if docs else 1)]] if causal and rng.random() < 0.5 else None
+    softcap = float(rng.choice([0.0, 0.0, 8.0, 30.0]))
+    slopes = rng.random(kvh * group).astype(np.float32) * np.float32(0.1) if rng.random() < 0.3 else None
+    q, k, v, dout = tensors = make(seed, 1, kvh * group, kvh, n, m, d, dtype)
+    for x in tensors:
+        if rng.random() < 0.5:
+            x[0, int(rng.integers(x.shape[1])), int(rng.integers(x.shape[2])), int(rng.integers(d))] = float(rng.choice([np.inf, -np.inf, np.nan]))
+    args = dict(causal=causal, doc_offsets=ints(docs), prefix=ints(prefix), softcap=softcap,
+                slopes=None if slopes is None else torch.from_numpy(slopes).to(DEV))
+    out, lse = lib.masked_attention(q, k, v, want_lse=True, **args)
+    got = dict(zip(("out", "lse", "dq", "dk", "dv"), (out, lse, *lib.masked_attention_backward(q, k, v, out, lse, dout, **args))))
+    torch.cuda.synchronize()
+    with np.errstate(all="ignore"):
+        want = by_formula(*(f64(x)[0] for x in tensors), mo.visible(1, n, m, causal, docs, prefix)[0], lib.resolved_scale(d), softcap, slopes)
+    for name, x in got.items():
+        x, r = f64(x)[0], want[name]
+        fin = np.isfinite(r)
+        assert np.array_equal(np.isfinite(x), fin), name
+        # norms: far above the roundings and far below what a lost row is worth; `rest` is for results that cancel to nothing
+        share, rest = (1e-2, 2.0 ** -6) if dtype == "bf16" else (1e-4, 2.0 ** -16)
+        assert np.linalg.norm(x[fin] - r[fin]) <= share * np.linalg.norm(r[fin]) + rest * np.sqrt(fin.sum()), name
