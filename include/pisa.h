@@ -295,7 +295,7 @@ typedef struct pisa_masked_shape {
  *   lse      fp32 [batch, heads, q_len], may be NULL
  *   workspace  pisa_masked_attention_workspace_bytes(shape) bytes, 16-byte aligned (may be NULL if that is 0): where there
  *            are few query rows their keys are shared out among workgroups and the parts joined from there
- * Two calls on different streams need a workspace each.
+ * Two calls on different streams need a workspace each.  Outputs share no memory with inputs, here and in the backward call.
  */
 size_t pisa_masked_attention_workspace_bytes(const pisa_masked_shape* shape);    /* 0 for an invalid shape as well */
 int32_t pisa_masked_attention(const pisa_masked_shape* shape, const void* q, const void* k, const void* v,

@@ -167,7 +167,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
   if (t_begin < t_end) load(t_begin, 0);
 
   u32x4 q[G::STEPS], g[G::STEPS];                // the lane's rows of q and dout; zeros where the row sees nothing
-  float delta = 0.f, minus_lse = -INFINITY;      // rows without a score above -inf: all weights 0
+  // Rows without a score above -inf have weights of 0, also those past the last: weights of 1, as rows of zeros would have, make
+  // their wave look for heavy keys in every tile (8 heads of 130 rows on 2 000 keys, backward 118 us, 76 so).
+  float delta = 0.f, minus_lse = -INFINITY;
   {
     const unsigned char* qs = p.q + b * p.sq.batch + head * p.sq.head + (long long)row * p.sq.token;
     const unsigned char* gsrc = p.dout + b * p.sdo.batch + head * p.sdo.head + (long long)row * p.sdo.token;
