@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || D == 64 ? 2 : 1) void masked
       }
       // Lane by lane, so that what a row gives does not hang on what its neighbours hold.  (The hint keeps this out of the way of
       // capped tiles: 24 heads of 4 608 tokens, capped and biased, 350 us without it, 324 with.)
-      if (__builtin_expect(far, 0)) {
+      if (__builtin_expect(far, !(MOD & CAP))) {
         if (MOD & CAP) {
           cap_scores<T>(s0, sc.to_cap, sc.cap);
           cap_scores<T>(s1, sc.to_cap, sc.cap);
